@@ -1,0 +1,468 @@
+"""Performance cases of the prompt encoder's operators, through the Python API.
+
+A scheduling decision starts at a prompt embedding; these are the operators
+that make one from token ids, and train the encoder that does:
+
+* ``embed``: embedding rows of tokens, scaled; per token, or pooled (sum or
+  mean) over the ragged prompts of a batch; ``embed_grad``: the gradient of
+  the table, by sorted tokens;
+* ``norm``: root-mean-square norm with the residual's addition, its output in
+  8 bits with a scale for each block of 128 columns or plain; ``norm_grad``:
+  its backward pass;
+* ``quantize``: 8-bit blocks with scales of activations (1 x 128), of weights
+  (128 x 128), and of their transposes;
+* ``matmul``: the product of 8-bit operands with those scales, plain or with
+  bias and ReLU; the forward product, and the two gradients' products.
+
+With ``own`` false the plain form runs: elementary torch operations in 32
+bits, rounded once. Inputs are drawn on the GPU from the seed: tokens by a
+Zipf law over a scattered vocabulary, prompt lengths lognormal (some prompts
+empty), activations normal with a few large columns.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+E4M3_MAX = 448.0
+MIN_SCALE = 2.0 ** -126
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}
+BYTES = {"f32": 4, "bf16": 2, "fp8": 1}
+
+
+def listed():
+    return [
+        # One arrival: the mean of one prompt's token embeddings. A few
+        # microseconds of work; launches count.
+        {"name": "embed_one_prompt", "kind": "embed", "T": 211, "Q": 1, "V": 32000, "d": 768, "type": "bf16",
+         "out": "bf16", "mean": True, "scale": 1.0, "pad": 0.0},
+        # The pending requests of 16 nodes (16,384 prompts of 64 tokens in the
+        # mean, from empty to thousands), pooled for the encoder.
+        {"name": "embed_16384_prompts", "kind": "embed", "T": 1048576, "Q": 16384, "V": 131072, "d": 1024,
+         "type": "bf16", "out": "bf16", "mean": True, "scale": 32.0, "pad": 0.0},
+        # A training step over 65,000 tokens that are looked up one by one: the
+        # dense gradient of a table whose sizes are multiples of nothing.
+        {"name": "embed_grad_tokens", "kind": "embed_grad", "T": 65000, "Q": 0, "V": 50021, "d": 768, "type": "bf16",
+         "mean": False, "scale": 27.7, "pad": 0.02, "add": False},
+        # A training step over pooled prompts, added to the gradient of the
+        # steps before.
+        {"name": "embed_grad_prompts", "kind": "embed_grad", "T": 524288, "Q": 4096, "V": 131072, "d": 1024,
+         "type": "f32", "mean": True, "scale": 32.0, "pad": 0.0, "add": True},
+        # The streaming workload's 8 arrivals: residual added, 8-bit output for
+        # the next product.
+        {"name": "norm_8_rows", "kind": "norm", "M": 8, "d": 768, "type": "bf16", "residual": True, "out": "fp8"},
+        # The same for the GEMM-bound workload's batch of 16,384.
+        {"name": "norm_16384", "kind": "norm", "M": 16384, "d": 1024, "type": "bf16", "residual": True, "out": "fp8"},
+        # Its backward pass in a training step, with the stream's own gradient.
+        {"name": "norm_grad_16384", "kind": "norm_grad", "M": 16384, "d": 1024, "type": "bf16", "stream": True},
+        # A weight matrix laid out once more after its update: 128 x 128 blocks.
+        {"name": "quantize_weight", "kind": "quantize", "M": 4096, "K": 1024, "type": "f32", "block": "square",
+         "transpose": False},
+        # A gradient of 16,001 rows for the weights' product: blocks along the
+        # rows, transposed.
+        {"name": "quantize_transposed", "kind": "quantize", "M": 16001, "K": 4096, "type": "bf16", "block": "row",
+         "transpose": True},
+        # 8 arrivals through a layer: one pass over the weights.
+        {"name": "matmul_8_rows", "kind": "matmul", "M": 8, "N": 4096, "K": 1024, "b": "square", "bias": True,
+         "relu": True, "out": "bf16"},
+        # 16,384 prompts through the same layer.
+        {"name": "matmul_16384", "kind": "matmul", "M": 16384, "N": 4096, "K": 1024, "b": "square", "bias": True,
+         "relu": True, "out": "bf16"},
+        # The layer's weight gradient: few tiles, a long sum over the prompts.
+        {"name": "matmul_weight_grad", "kind": "matmul", "M": 4096, "N": 1024, "K": 16384, "b": "row", "bias": False,
+         "relu": False, "out": "f32"},
+    ]
+
+
+# --------------------------------------------------------------------- draws
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _width(rng, hi):
+    """A row length: a configuration's, or one of any residue."""
+    d = rng.choice([128, 384, 768, 1024, 2048, 4096, _log_int(rng, 32, 4096), _log_int(rng, 32, 4096)])
+    return min(d, hi)
+
+
+def draw(rng):
+    kind = rng.choice(["embed", "embed", "embed_grad", "embed_grad", "norm", "norm", "norm_grad", "quantize", "quantize",
+                       "matmul", "matmul", "matmul"])
+    if kind in ("embed", "embed_grad"):
+        most = (1 << 30) if kind == "embed" else (1 << 28)
+        d = _width(rng, 4096)
+        V = _log_int(rng, 1000, min(262144, (1 << 27) // d))
+        T = _log_int(rng, 1, min(1 << 20, most // d))
+        Q = rng.choice([0, 1, _log_int(rng, 1, max(1, min(T, 16384))), _log_int(rng, 1, max(1, min(T, 16384)))])
+        case = {"kind": kind, "T": T, "Q": Q, "V": V, "d": d, "type": rng.choice(["bf16", "bf16", "f32"]),
+                "mean": bool(Q) and rng.random() < 0.5,
+                "scale": rng.choice([1.0, round(math.sqrt(d), 3), 0.5]), "pad": rng.choice([0.0, 0.0, 0.05])}
+        if kind == "embed":
+            case["out"] = rng.choice([case["type"], "f32", "bf16"])
+            if Q == 0:
+                case["T"] = min(T, (1 << 29) // d)
+        else:
+            case["add"] = rng.random() < 0.4
+        return case
+    if kind in ("norm", "norm_grad"):
+        d = _width(rng, 4096) if rng.random() < 0.8 else _log_int(rng, 4096, 16384)
+        M = _log_int(rng, 1, (1 << 24) // d)
+        t = rng.choice(["bf16", "bf16", "f32"])
+        if kind == "norm":
+            return {"kind": kind, "M": M, "d": d, "type": t, "residual": rng.random() < 0.7,
+                    "out": rng.choice(["fp8", "fp8", "bf16", "f32"])}
+        return {"kind": kind, "M": M, "d": d, "type": t, "stream": rng.random() < 0.6}
+    if kind == "quantize":
+        K = _log_int(rng, 32, 8192) if rng.random() < 0.5 else rng.choice([384, 768, 1024, 4096])
+        return {"kind": kind, "M": _log_int(rng, 1, (1 << 26) // K), "K": K, "type": rng.choice(["bf16", "bf16", "f32"]),
+                "block": rng.choice(["row", "row", "square"]), "transpose": rng.random() < 0.5}
+    b = rng.choice(["square", "square", "row"])
+    K = rng.choice([384, 768, 1024, 2048, 4096, 16 * _log_int(rng, 2, 1024)])
+    N = rng.choice([384, 768, 1024, 4096, _log_int(rng, 16, 8192)])
+    M = _log_int(rng, 1, max(1, min(16384, (1 << 36) // (N * K))))
+    return {"kind": kind, "M": M, "N": N, "K": K, "b": b, "bias": rng.random() < 0.5, "relu": rng.random() < 0.3,
+            "out": rng.choice(["bf16", "bf16", "f32"])}
+
+
+# -------------------------------------------------------------------- inputs
+def _tokens(case, g):
+    """Zipf (rank r with probability ~ 1/r) over ids scattered by a product modulo V."""
+    T, V = case["T"], case["V"]
+    u = torch.rand(T, generator=g, device=DEV, dtype=torch.float64)
+    rank = (torch.exp(u * math.log(V + 1)) - 1).long().clamp_(0, V - 1)
+    ids = (rank * 2654435761 + 12345) % V
+    if case["pad"]:
+        ids = torch.where(torch.rand(T, generator=g, device=DEV) < case["pad"], torch.full_like(ids, -1), ids)
+    return ids.to(torch.int32)
+
+
+def _offsets(case, g):
+    """Q prompts over the T tokens: lognormal lengths, some of them empty."""
+    T, Q = case["T"], case["Q"]
+    if Q == 0:
+        return None
+    w = torch.exp(1.0 * torch.randn(Q, generator=g, device=DEV, dtype=torch.float64))
+    if Q > 8:
+        w = w * (torch.rand(Q, generator=g, device=DEV) > 0.01)
+        w[0] += 1e-3
+    cut = torch.cumsum(w, 0)
+    cut = torch.round(cut / cut[-1] * T).to(torch.int32)
+    cut[-1] = T
+    return torch.cat([torch.zeros(1, dtype=torch.int32, device=DEV), cut])
+
+
+def _rows(M, d, dtype, g, spread=True):
+    """Normal activations, a few columns of them ten times as large."""
+    x = torch.randn(M, d, generator=g, device=DEV)
+    if spread:
+        big = torch.rand(d, generator=g, device=DEV) < 0.02
+        x *= torch.where(big, 10.0, 1.0)
+    return x.to(TYPES[dtype])
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    k = case["kind"]
+    s = {"case": case}
+    if k == "embed":
+        s["tokens"], s["offsets"] = _tokens(case, g), _offsets(case, g)
+        s["table"] = (0.02 * torch.randn(case["V"], case["d"], generator=g, device=DEV)).to(TYPES[case["type"]])
+    elif k == "embed_grad":
+        s["tokens"], s["offsets"] = _tokens(case, g), _offsets(case, g)
+        s["grad"] = _rows(case["Q"] or case["T"], case["d"], case["type"], g)
+        s["held"] = torch.randn(case["V"], case["d"], generator=g, device=DEV) if case["add"] else None
+    elif k == "norm":
+        s["x"] = _rows(case["M"], case["d"], case["type"], g)
+        s["residual"] = _rows(case["M"], case["d"], case["type"], g) if case["residual"] else None
+        s["gain"] = 1.0 + 0.1 * torch.randn(case["d"], generator=g, device=DEV)
+    elif k == "norm_grad":
+        s["total"] = _rows(case["M"], case["d"], case["type"], g)
+        s["grad"] = _rows(case["M"], case["d"], case["type"], g, spread=False)
+        s["stream"] = _rows(case["M"], case["d"], case["type"], g, spread=False) if case["stream"] else None
+        s["gain"] = 1.0 + 0.1 * torch.randn(case["d"], generator=g, device=DEV)
+    elif k == "quantize":
+        s["x"] = _rows(case["M"], case["K"], case["type"], g)
+    else:
+        M, N, K = case["M"], case["N"], case["K"]
+        s["a"], s["a_scales"] = _plain_quantize(_rows(M, K, "f32", g), "row", False)
+        s["b"], s["b_scales"] = _plain_quantize(_rows(N, K, "f32", g, spread=False) / math.sqrt(K), case["b"], False)
+        s["bias"] = 0.1 * torch.randn(N, generator=g, device=DEV) if case["bias"] else None
+    return s
+
+
+# ---------------------------------------------------------------- plain forms
+def _plain_quantize(x, block, transpose):
+    """8-bit values [R, C padded to 16] and scales [ceil(C / 128), R or ceil(R / 128)]."""
+    x = x.float()
+    if transpose:
+        x = x.t()
+    R, C = x.shape
+    kb, rb = -(-C // 128), -(-R // 128)
+    padded = torch.nn.functional.pad(x, (0, 128 * kb - C))
+    mag = padded.abs()
+    mag = torch.where(mag <= torch.finfo(torch.float32).max, mag, torch.zeros_like(mag))   # what is not finite counts not
+    amax = mag.view(R, kb, 128).amax(2)
+    if block == "square":
+        amax = torch.nn.functional.pad(amax, (0, 0, 0, 128 * rb - R)).view(rb, 128, kb).amax(1)
+    scales = (amax / E4M3_MAX).clamp_min(MIN_SCALE)
+    inv = 1.0 / scales
+    inv = inv.repeat_interleave(128, 0)[:R] if block == "square" else inv
+    q = (padded.view(R, kb, 128) * inv[:, :, None]).view(R, 128 * kb)
+    return q[:, :16 * (-(-C // 16))].to(torch.float8_e4m3fn).contiguous(), scales.t().contiguous()
+
+
+def _prompt_of(offsets, T):
+    return torch.searchsorted(offsets[1:].contiguous(), torch.arange(T, dtype=torch.int32, device=DEV), right=True)
+
+
+def _plain_embed(tokens, table, scale, offsets, mean, dtype):
+    valid = (tokens >= 0) & (tokens < table.shape[0])
+    rows = table[torch.where(valid, tokens, torch.zeros_like(tokens))].float() * valid[:, None]
+    if offsets is None:
+        return (rows * scale).to(dtype)
+    bag, Q = _prompt_of(offsets, tokens.shape[0]), offsets.shape[0] - 1
+    total = torch.zeros(Q, table.shape[1], device=DEV).index_add_(0, bag, rows)
+    if mean:
+        n = torch.zeros(Q, device=DEV).index_add_(0, bag, valid.float())
+        total = total / n.clamp_min(1.0)[:, None]
+    return (total * scale).to(dtype)
+
+
+def _plain_embed_grad(tokens, grad, scale, offsets, mean, V, held):
+    valid = (tokens >= 0) & (tokens < V)
+    g = grad.float() * scale
+    if offsets is None:
+        rows = g
+    else:
+        bag = _prompt_of(offsets, tokens.shape[0])
+        if mean:
+            n = torch.zeros(offsets.shape[0] - 1, device=DEV).index_add_(0, bag, valid.float())
+            g = g / n.clamp_min(1.0)[:, None]
+        rows = g[bag]
+    rows = rows * valid[:, None]
+    if held is None:
+        held = torch.zeros(V, grad.shape[1], device=DEV)
+    return held.index_add(0, torch.where(valid, tokens, torch.zeros_like(tokens)), rows)
+
+
+def _plain_norm(x, gain, residual, out, eps=1e-6):
+    s = x.float() if residual is None else x.float() + residual.float()
+    n = s * torch.rsqrt((s * s).mean(1, keepdim=True) + eps) * gain
+    total = None if residual is None else s.to(x.dtype)
+    if out == "fp8":
+        q, scales = _plain_quantize(n, "row", False)
+        return q, scales, total
+    return n.to(TYPES[out]), None, total
+
+
+def _plain_norm_grad(grad, total, gain, stream, eps=1e-6):
+    s, dy = total.float(), grad.float()
+    w = torch.rsqrt((s * s).mean(1, keepdim=True) + eps)
+    u = dy * gain
+    dx = w * u - s * (w * w * w) * (u * s).mean(1, keepdim=True)
+    if stream is not None:
+        dx = dx + stream.float()
+    return dx.to(total.dtype), (dy * s * w).sum(0)
+
+
+def _spread(scales, rows, cols, square):
+    full = scales.t().repeat_interleave(128, 1)[:, :cols]
+    return full.repeat_interleave(128, 0)[:rows] if square else full
+
+
+def _plain_matmul(a, a_scales, b, b_scales, square, bias, relu, dtype):
+    x = a.float() * _spread(a_scales, a.shape[0], a.shape[1], False)
+    w = b.float() * _spread(b_scales, b.shape[0], b.shape[1], square)
+    y = x @ w.t()
+    if bias is not None:
+        y = y + bias
+    if relu:
+        y = y.clamp_min(0.0)
+    return y.to(dtype)
+
+
+def run(state):
+    case = state["case"]
+    k = case["kind"]
+    if own:
+        from paper_2603_07917_amd import sage
+        if k == "embed":
+            return sage.embed(state["tokens"], state["table"], scale=case["scale"], offsets=state["offsets"],
+                              mean=case["mean"], dtype=TYPES[case["out"]])
+        if k == "embed_grad":
+            return sage.embed_grad(state["tokens"], state["grad"], case["V"], scale=case["scale"],
+                                   offsets=state["offsets"], mean=case["mean"], add=state["held"])
+        if k == "norm":
+            y, scales, total = sage.rms_norm(state["x"], state["gain"], residual=state["residual"],
+                                             dtype=TYPES[case["out"]])
+            return {n: v for n, v in (("y", y), ("scales", scales), ("total", total)) if v is not None}
+        if k == "norm_grad":
+            dx, dgain = sage.rms_norm_grad(state["grad"], state["total"], state["gain"], grad_total=state["stream"])
+            return {"grad_x": dx, "grad_gain": dgain}
+        if k == "quantize":
+            q, scales = sage.quantize(state["x"], block=case["block"], transpose=case["transpose"])
+            return {"q": q, "scales": scales}
+        return sage.matmul_fp8(state["a"], state["a_scales"], state["b"], state["b_scales"], bias=state["bias"],
+                               relu=case["relu"], dtype=TYPES[case["out"]])
+    if k == "embed":
+        return _plain_embed(state["tokens"], state["table"], case["scale"], state["offsets"], case["mean"],
+                            TYPES[case["out"]])
+    if k == "embed_grad":
+        return _plain_embed_grad(state["tokens"], state["grad"], case["scale"], state["offsets"], case["mean"],
+                                 case["V"], state["held"])
+    if k == "norm":
+        y, scales, total = _plain_norm(state["x"], state["gain"], state["residual"], case["out"])
+        return {n: v for n, v in (("y", y), ("scales", scales), ("total", total)) if v is not None}
+    if k == "norm_grad":
+        dx, dgain = _plain_norm_grad(state["grad"], state["total"], state["gain"], state["stream"])
+        return {"grad_x": dx, "grad_gain": dgain}
+    if k == "quantize":
+        q, scales = _plain_quantize(state["x"], case["block"], case["transpose"])
+        return {"q": q, "scales": scales}
+    return _plain_matmul(state["a"], state["a_scales"], state["b"], state["b_scales"], case["b"] == "square",
+                         state["bias"], case["relu"], TYPES[case["out"]])
+
+
+# ---------------------------------------------------------- 64-bit definitions
+def _bags64(case, offsets):
+    """Index of every token's prompt, by repetition of the lengths."""
+    lens = (offsets[1:] - offsets[:-1]).long()
+    return torch.repeat_interleave(torch.arange(case["Q"], device=DEV), lens)
+
+
+def _blocks64(v, block):
+    """What an 8-bit value stands for before its rounding (v / scale, zero-padded
+    to 16 columns) and the scales, of a 64-bit matrix."""
+    R, C = v.shape
+    kb, rb = (C + 127) // 128, (R + 127) // 128
+    scales = torch.empty(kb, R if block == "row" else rb, dtype=torch.float64, device=DEV)
+    q = torch.zeros(R, 16 * ((C + 15) // 16), dtype=torch.float64, device=DEV)
+    for j in range(kb):
+        part = v[:, 128 * j:min(C, 128 * j + 128)]
+        top = part.abs().max(1).values
+        if block == "square":
+            top = torch.cat([top, top.new_zeros(128 * rb - R)]).reshape(rb, 128).max(1).values
+        scales[j] = torch.maximum(top / E4M3_MAX, torch.full_like(top, MIN_SCALE))
+        per_row = scales[j] if block == "row" else scales[j][torch.arange(R, device=DEV) // 128]
+        q[:, 128 * j:128 * j + part.shape[1]] = part / per_row[:, None]
+    return q, scales
+
+
+def exact(case, seed):
+    """The definitions in 64 bits. An 8-bit output's value is the one before
+    its rounding to 8 bits: the rounding is how the result is kept."""
+    s = prepare(case, seed)
+    k = case["kind"]
+    if k == "embed":
+        tok, table = s["tokens"].long(), s["table"].double() * case["scale"]
+        ok = (tok >= 0) & (tok < case["V"])
+        if s["offsets"] is None:
+            out = torch.zeros(case["T"], case["d"], dtype=torch.float64, device=DEV)
+            out[ok] = table[tok[ok]]
+            return out
+        bag = _bags64(case, s["offsets"])
+        out = torch.zeros(case["Q"], case["d"], dtype=torch.float64, device=DEV)
+        for i in range(0, case["T"], 262144):
+            part = ok[i:i + 262144]
+            out.index_add_(0, bag[i:i + 262144][part], table[tok[i:i + 262144][part]])
+        if case["mean"]:
+            n = torch.bincount(bag[ok], minlength=case["Q"]).double()
+            out /= torch.where(n > 0, n, torch.ones_like(n))[:, None]
+        return out
+    if k == "embed_grad":
+        tok, g = s["tokens"].long(), s["grad"].double() * case["scale"]
+        ok = (tok >= 0) & (tok < case["V"])
+        src = torch.arange(case["T"], device=DEV)
+        if s["offsets"] is not None:
+            src = _bags64(case, s["offsets"])
+            if case["mean"]:
+                n = torch.bincount(src[ok], minlength=case["Q"]).double()
+                g = g / torch.where(n > 0, n, torch.ones_like(n))[:, None]
+        out = s["held"].double() if case["add"] else torch.zeros(case["V"], case["d"], dtype=torch.float64, device=DEV)
+        for i in range(0, case["T"], 262144):
+            part = ok[i:i + 262144]
+            out.index_add_(0, tok[i:i + 262144][part], g[src[i:i + 262144][part]])
+        return out
+    if k == "norm":
+        t = s["x"].double()
+        if s["residual"] is not None:
+            t = t + s["residual"].double()
+        n = t / torch.sqrt(t.pow(2).sum(1) / case["d"] + 1e-6)[:, None] * s["gain"].double()
+        out = {}
+        if case["out"] == "fp8":
+            out["y"], out["scales"] = _blocks64(n, "row")
+        else:
+            out["y"] = n
+        if s["residual"] is not None:
+            out["total"] = t
+        return out
+    if k == "norm_grad":
+        t, dy, gain = s["total"].double(), s["grad"].double(), s["gain"].double()
+        rms = torch.sqrt(t.pow(2).sum(1) / case["d"] + 1e-6)[:, None]
+        unit = t / rms
+        u = dy * gain
+        dx = (u - unit * ((u * unit).sum(1) / case["d"])[:, None]) / rms
+        if s["stream"] is not None:
+            dx = dx + s["stream"].double()
+        return {"grad_x": dx, "grad_gain": (dy * unit).sum(0)}
+    if k == "quantize":
+        x = s["x"].double()
+        q, scales = _blocks64(x.t() if case["transpose"] else x, case["block"])
+        return {"q": q, "scales": scales}
+    out = torch.zeros(case["M"], case["N"], dtype=torch.float64, device=DEV)
+    for j in range((case["K"] + 127) // 128):
+        a = s["a"][:, 128 * j:128 * j + 128].double() * s["a_scales"][j].double()[:, None]
+        sb = s["b_scales"][j].double()
+        if case["b"] == "square":
+            sb = sb[torch.arange(case["N"], device=DEV) // 128]
+        b = s["b"][:, 128 * j:128 * j + 128].double() * sb[:, None]
+        out += a @ b.t().contiguous()
+    if s["bias"] is not None:
+        out += s["bias"].double()
+    return torch.relu(out) if case["relu"] else out
+
+
+def work(case):
+    k = case["kind"]
+    if k in ("embed", "embed_grad"):
+        T, Q, V, d, e = case["T"], case["Q"], case["V"], case["d"], BYTES[case["type"]]
+        # Zipf tokens: about this many of the V rows are met at all
+        met = V if T > 40 * V else min(V, T, sum_met(T, V))
+        if k == "embed":
+            b = 4 * T + met * d * e + (Q or T) * d * BYTES[case["out"]]
+        else:
+            b = 4 * T + (Q or T) * d * e + V * d * 4 + (V * d * 4 if case["add"] else 0)
+        return {"bytes": b + 4 * Q, "flops": T * d}
+    if k == "norm":
+        M, d, e = case["M"], case["d"], BYTES[case["type"]]
+        n = M * d
+        b = n * e * (3 if case["residual"] else 1) + n * BYTES[case["out"]] + 4 * d
+        b += 4 * M * -(-d // 128) if case["out"] == "fp8" else 0
+        return {"bytes": b, "flops": 6 * n}
+    if k == "norm_grad":
+        n = case["M"] * case["d"]
+        return {"bytes": n * BYTES[case["type"]] * (4 if case["stream"] else 3) + 8 * case["d"], "flops": 10 * n}
+    if k == "quantize":
+        n = case["M"] * case["K"]
+        return {"bytes": n * (BYTES[case["type"]] + 1) + n // (32 if case["block"] == "row" else 4096), "flops": 3 * n}
+    M, N, K = case["M"], case["N"], case["K"]
+    kb = -(-K // 128)
+    b = M * K + N * K + 4 * kb * (M + (N if case["b"] == "row" else -(-N // 128))) + M * N * BYTES[case["out"]]
+    return {"bytes": b + (4 * N if case["bias"] else 0), "flops": 2 * M * N * K}
+
+
+def sum_met(T, V):
+    """Expected number of distinct ids among T draws of the Zipf law over V."""
+    total, lo = 0.0, 1
+    h = math.log(V + 1)
+    while lo <= V:                                       # ranks in growing groups
+        hi = min(V, lo + lo // 8)
+        p = (math.log(hi + 1) - math.log(lo)) / h / (hi - lo + 1)
+        total += (hi - lo + 1) * (1.0 - math.exp(-T * p))
+        lo = hi + 1
+    return int(total) + 1
