@@ -68,13 +68,14 @@ def listed():
          "transpose": True},
         # 8 arrivals through a layer: one pass over the weights.
         {"name": "matmul_8_rows", "kind": "matmul", "M": 8, "N": 4096, "K": 1024, "b": "square", "bias": True,
-         "relu": True, "out": "bf16"},
-        # 16,384 prompts through the same layer.
+         "relu": True, "out": "bf16", "fast": False},
+        # 16,384 prompts through the same layer, the sums of products that a
+        # bf16 output does not resolve left to the 8-bit matrix instructions.
         {"name": "matmul_16384", "kind": "matmul", "M": 16384, "N": 4096, "K": 1024, "b": "square", "bias": True,
-         "relu": True, "out": "bf16"},
+         "relu": True, "out": "bf16", "fast": True},
         # The layer's weight gradient: few tiles, a long sum over the prompts.
         {"name": "matmul_weight_grad", "kind": "matmul", "M": 4096, "N": 1024, "K": 16384, "b": "row", "bias": False,
-         "relu": False, "out": "f32"},
+         "relu": False, "out": "f32", "fast": False},
     ]
 
 
@@ -124,8 +125,9 @@ def draw(rng):
     K = rng.choice([384, 768, 1024, 2048, 4096, 16 * _log_int(rng, 2, 1024)])
     N = rng.choice([384, 768, 1024, 4096, _log_int(rng, 16, 8192)])
     M = _log_int(rng, 1, max(1, min(16384, (1 << 36) // (N * K))))
+    out = rng.choice(["bf16", "bf16", "f32"])
     return {"kind": kind, "M": M, "N": N, "K": K, "b": b, "bias": rng.random() < 0.5, "relu": rng.random() < 0.3,
-            "out": rng.choice(["bf16", "bf16", "f32"])}
+            "out": out, "fast": out == "bf16" and rng.random() < 0.6}
 
 
 # -------------------------------------------------------------------- inputs
@@ -308,7 +310,7 @@ def run(state):
             q, scales = sage.quantize(state["x"], block=case["block"], transpose=case["transpose"])
             return {"q": q, "scales": scales}
         return sage.matmul_fp8(state["a"], state["a_scales"], state["b"], state["b_scales"], bias=state["bias"],
-                               relu=case["relu"], dtype=TYPES[case["out"]])
+                               relu=case["relu"], fast_accum=case["fast"], dtype=TYPES[case["out"]])
     if k == "embed":
         return _plain_embed(state["tokens"], state["table"], case["scale"], state["offsets"], case["mean"],
                             TYPES[case["out"]])
