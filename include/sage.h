@@ -529,6 +529,154 @@ int sage_simulate(const double* arrival, const int32_t* prompt_len, const int32_
                   const int32_t* order, int levels, int informed, int bucket, int servers, double rate,
                   int queue_cap, double* finish, int32_t* preemptions);
 
+/*
+ * Operators of a prompt encoder (Sec. 3.1 compares prompts by the embeddings
+ * that one makes of them): from token ids to the unit-norm embeddings that
+ * sage_predict and sage_decide take, and the gradients to train it.
+ *
+ * Element types: SAGE_F32, SAGE_BF16 (raw 16-bit patterns), SAGE_E4M3 (8-bit
+ * floating point, 4 exponent and 3 mantissa bits, largest value 448, no
+ * infinities). All sums, statistics and gradients are accumulated in fp32;
+ * each output is rounded once, to nearest even.
+ *
+ * 8-bit matrices: a matrix of R rows and C columns is stored as e4m3 bytes
+ * [R, C16], C16 = C rounded up to a multiple of 16, the added columns zero,
+ * with fp32 scales for each block of 128 columns (the last one may be
+ * shorter):
+ *   SAGE_BLOCK_ROW     per row:      scales [ceil(C / 128), R]
+ *   SAGE_BLOCK_SQUARE  per 128 rows: scales [ceil(C / 128), ceil(R / 128)]
+ * Element (r, c) stands for q[r, c] * scale of its block. A block's scale is
+ * max(amax / 448, 2^-126), amax the largest magnitude of its finite values,
+ * and q = e4m3(x * (1 / scale)). An infinity or NaN becomes a NaN and leaves
+ * the other values of its block as they are.
+ */
+enum { SAGE_F32 = 0, SAGE_BF16 = 1, SAGE_E4M3 = 2 };
+enum { SAGE_BLOCK_ROW = 0, SAGE_BLOCK_SQUARE = 1 };
+#define SAGE_MAX_NORM_COLS 32768
+
+/*
+ * sage_embed - rows of an embedding table, scaled; one per token, or pooled
+ * over the tokens of each prompt.
+ *   tokens [T] int32    token ids; one outside [0, V) is no token: it adds
+ *                       nothing (a row of zeros where each has its own)
+ *   table [V, d]        table_type SAGE_F32 or SAGE_BF16
+ *   offsets [Q+1] int32 prompt q is tokens[offsets[q] .. offsets[q+1]);
+ *                       non-decreasing, within [0, T] (not checked before
+ *                       enqueue: device array). Tokens before offsets[0] and
+ *                       from offsets[Q] on are in no prompt. NULL: no prompts,
+ *                       Q is ignored
+ *   mean                non-zero: divide by the prompt's number of valid
+ *                       tokens (needs offsets)
+ *   out [T, d], with offsets [Q, d]   out_type SAGE_F32 or SAGE_BF16:
+ *                       scale * row, scale * (sum or mean); zeros for a prompt
+ *                       with no valid token
+ *   workspace           >= sage_embed_workspace_bytes(T, Q, d) bytes with
+ *                       offsets; none without
+ * A prompt's rows are added in an order that depends on the sizes alone.
+ * SAGE_EINVAL: T, Q outside [0, 2^30], V outside [1, 2^30], d outside
+ * [1, 2^20], a scale that is not finite, unknown types, a mean without
+ * offsets, NULL or misaligned pointers, out overlapping the table. T = 0 with
+ * prompts gives zeros; no output rows is a no-op.
+ */
+size_t sage_embed_workspace_bytes(int T, int Q, int d);
+int sage_embed(const int32_t* tokens, int T, const void* table, int table_type, int V, int d, float scale,
+               const int32_t* offsets, int Q, int mean, void* out, int out_type,
+               void* workspace, size_t workspace_bytes, sage_stream_t stream);
+
+/*
+ * sage_embed_grad - gradient of sage_embed with respect to the table:
+ *   out[v] = add[v] + scale * sum over the tokens t = v of grad[row of t],
+ * each divided by its prompt's number of valid tokens for a mean. The tokens
+ * are sorted, and the rows of one token added in an order that depends on
+ * the inputs alone (no atomics on values: repeated calls give the same bits).
+ *   grad [T, d], with offsets [Q, d]   grad_type SAGE_F32 or SAGE_BF16
+ *   add [V, d] f32 or NULL (zeros); may be out itself: the gradient is then
+ *                       added in place, and rows of tokens that are not in
+ *                       the batch are not touched
+ *   out [V, d] f32; other arguments as in sage_embed
+ *   workspace           >= sage_embed_grad_workspace_bytes(T, Q, V, d) bytes
+ *                       (Q = 0 without offsets)
+ * Errors as in sage_embed; SAGE_EINVAL also when out overlaps grad, or add in
+ * part. T = 0 copies add.
+ */
+size_t sage_embed_grad_workspace_bytes(int T, int Q, int V, int d);
+int sage_embed_grad(const int32_t* tokens, int T, const void* grad, int grad_type, int V, int d, float scale,
+                    const int32_t* offsets, int Q, int mean, const float* add, float* out,
+                    void* workspace, size_t workspace_bytes, sage_stream_t stream);
+
+/*
+ * sage_rms_norm - root-mean-square norm of s = x + residual:
+ *   out = s * (mean(s^2) + eps)^(-1/2) * gain   per row of d columns.
+ *   x, residual [M, d]  `type` SAGE_F32 or SAGE_BF16; residual may be NULL
+ *   gain [d] f32, eps >= 0
+ *   total [M, d] or NULL  s, rounded to `type` (the norm is taken of the
+ *                       unrounded s); may be x or residual itself
+ *   out [M, d]          SAGE_F32 or SAGE_BF16; SAGE_E4M3: an 8-bit matrix with
+ *                       SAGE_BLOCK_ROW scales, out [M, d16] and scales
+ *                       [ceil(d / 128), M] (else scales is ignored)
+ * With gain = 1 / sqrt(d) the output has unit norm. SAGE_EINVAL: M outside
+ * [0, 2^30], d outside [1, SAGE_MAX_NORM_COLS], eps negative or not finite,
+ * unknown types, NULL or misaligned pointers, overlapping buffers other than
+ * the two above. M = 0 is a no-op.
+ */
+int sage_rms_norm(const void* x, const void* residual, int type, int M, int d, const float* gain, float eps,
+                  void* total, void* out, int out_type, float* scales, sage_stream_t stream);
+
+/*
+ * sage_rms_norm_grad - backward pass of sage_rms_norm, from the stored s:
+ * with w = (mean(s^2) + eps)^(-1/2) and u = gain * grad per row,
+ *   grad_x = w u - s w^3 mean(u s) + grad_total   (also the residual's)
+ *   grad_gain = sum over rows of grad s w
+ *   grad, total, grad_total, grad_x [M, d] of `type`; grad_total (the
+ *   gradient that reaches s by the residual stream) may be NULL; grad_x may be
+ *   one of the inputs; grad_gain [d] f32
+ *   workspace >= sage_rms_norm_grad_workspace_bytes(M, d) bytes
+ * An 8-bit output counts as its unrounded values. Errors as in sage_rms_norm.
+ * M = 0 gives a zero grad_gain.
+ */
+size_t sage_rms_norm_grad_workspace_bytes(int M, int d);
+int sage_rms_norm_grad(const void* grad, const void* total, int type, int M, int d, const float* gain, float eps,
+                       const void* grad_total, void* grad_x, float* grad_gain,
+                       void* workspace, size_t workspace_bytes, sage_stream_t stream);
+
+/*
+ * sage_quantize - an 8-bit matrix from x [M, K] (SAGE_F32 or SAGE_BF16), or,
+ * with `transpose`, from its transpose: q [M, K16] (transpose: [K, M16]) and
+ * scales for SAGE_BLOCK_ROW or SAGE_BLOCK_SQUARE, as described above.
+ * SAGE_EINVAL: unknown type or block, M or K outside [0, 2^30], M *
+ * ceil(K / 128) not below 2^28, NULL or misaligned pointers, q overlapping x.
+ * M = 0 or K = 0 is a no-op.
+ */
+int sage_quantize(const void* x, int type, int M, int K, int block, int transpose, uint8_t* q, float* scales,
+                  sage_stream_t stream);
+
+/*
+ * sage_matmul_fp8 - product of 8-bit matrices:
+ *   out[m, n] = sum over k of a[m, k] b[n, k] (the values they stand for)
+ *               + bias[n], negative results to 0 with `relu`.
+ *   a [M, K] e4m3, a_scales [ceil(K / 128), M] (SAGE_BLOCK_ROW)
+ *   b [N, K] e4m3, b_scales as b_block says; K is the stored row length, a
+ *   multiple of 16 in [16, 2^20]
+ *   bias [N] f32 or NULL; out [M, N] SAGE_F32 or SAGE_BF16
+ *   fast_accum  0: exact products, fp32 sums. Otherwise the 8-bit matrix
+ *               instructions, at twice the rate: products are added in groups
+ *               of 8 with about 13 bits below a group's largest (an error of
+ *               about 1.4e-5 of the results' size on normal data, far below
+ *               the rounding of a bf16 output), the groups in fp32
+ *   workspace >= sage_matmul_fp8_workspace_bytes(M, N, K) bytes (0 for many
+ *   sizes)
+ * A layer y = x W^T has a = x in rows, b = W in squares; its gradients are
+ * the same product: grad_x from a = grad_y, b = W transposed; grad_W from
+ * a = grad_y transposed and b = x transposed, both in rows.
+ * SAGE_EINVAL: sizes, 2^22 tiles of 128 x 128 outputs or more, unknown types,
+ * NULL or misaligned pointers, out overlapping an operand; SAGE_EWORKSPACE.
+ * M = 0 or N = 0 is a no-op.
+ */
+size_t sage_matmul_fp8_workspace_bytes(int M, int N, int K);
+int sage_matmul_fp8(const uint8_t* a, const float* a_scales, int M, const uint8_t* b, const float* b_scales,
+                    int b_block, int N, int K, const float* bias, int relu, int fast_accum,
+                    void* out, int out_type, void* workspace, size_t workspace_bytes, sage_stream_t stream);
+
 /* Static, thread-safe name of a status code. Host pointer. */
 const char* sage_status_string(int status);
 

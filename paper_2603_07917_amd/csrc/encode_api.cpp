@@ -1,0 +1,254 @@
+// C ABI of the prompt encoder's operators: argument validation, workspace
+// sizes and dispatch. Nothing here allocates device memory.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "sage.h"
+#include "sage_api.hpp"
+#include "sage_encode.hpp"
+
+using sage::aligned16;
+using sage::check_device;
+using sage::fail;
+using sage::hip_status;
+using sage::ok;
+
+namespace {
+
+constexpr int kMaxTokens = 1 << 30;
+constexpr int kMaxRows = 1 << 30;
+constexpr int kMaxCols = 1 << 20;                       // of an embedding, and of an 8-bit operand: byte offsets of
+                                                        // 256 rows of one stay within 32 bits
+
+bool is_row_type(int t) { return t == SAGE_F32 || t == SAGE_BF16; }
+
+struct Arg {
+  const void* p;
+  const char* name;
+  bool optional;
+};
+template <size_t n>
+int check_pointers(const char* fn, const Arg (&args)[n]) {
+  for (const Arg& a : args) {
+    if (!a.p && !a.optional) return fail(SAGE_EINVAL, "%s: %s is NULL", fn, a.name);
+    if (!aligned16(a.p)) return fail(SAGE_EINVAL, "%s: %s is not 16-byte aligned", fn, a.name);
+  }
+  return SAGE_OK;
+}
+int check_workspace(const char* fn, const void* ws, size_t have, size_t need) {
+  if (need == 0) return SAGE_OK;
+  if (!ws || have < need) return fail(SAGE_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, have, need);
+  if (!aligned16(ws)) return fail(SAGE_EINVAL, "%s: workspace is not 16-byte aligned", fn);
+  return SAGE_OK;
+}
+// Whether [a, a + na) and [b, b + nb) share a byte.
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + nb && y < x + na;
+}
+size_t type_bytes(int t) { return t == SAGE_F32 ? 4 : t == SAGE_BF16 ? 2 : 1; }
+
+int check_embed_sizes(const char* fn, int T, int V, int d, float scale, bool prompts, int Q) {
+  if (T < 0 || T > kMaxTokens) return fail(SAGE_EINVAL, "%s: T=%d outside [0, 2^30]", fn, T);
+  if (V < 1 || V > kMaxRows) return fail(SAGE_EINVAL, "%s: V=%d outside [1, 2^30]", fn, V);
+  if (d < 1 || d > kMaxCols) return fail(SAGE_EINVAL, "%s: d=%d outside [1, 2^20]", fn, d);
+  if (prompts && (Q < 0 || Q > kMaxRows)) return fail(SAGE_EINVAL, "%s: Q=%d outside [0, 2^30]", fn, Q);
+  if (!std::isfinite(scale)) return fail(SAGE_EINVAL, "%s: scale is not finite", fn);
+  return SAGE_OK;
+}
+bool embed_sizes_ok(int T, int Q, int d) {
+  return T >= 0 && T <= kMaxTokens && Q >= 0 && Q <= kMaxRows && d >= 1 && d <= kMaxCols;
+}
+int check_norm_sizes(const char* fn, int type, int M, int d, float eps) {
+  if (!is_row_type(type)) return fail(SAGE_EINVAL, "%s: type=%d is not SAGE_F32 or SAGE_BF16", fn, type);
+  if (M < 0 || M > kMaxRows) return fail(SAGE_EINVAL, "%s: M=%d outside [0, 2^30]", fn, M);
+  if (d < 1 || d > SAGE_MAX_NORM_COLS) return fail(SAGE_EINVAL, "%s: d=%d outside [1, %d]", fn, d, SAGE_MAX_NORM_COLS);
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(SAGE_EINVAL, "%s: eps must be finite and >= 0", fn);
+  return SAGE_OK;
+}
+static_assert(SAGE_MAX_NORM_COLS == sage::kMaxNormCols, "the header's limit is the kernels'");
+static_assert(SAGE_F32 == sage::kF32 && SAGE_BF16 == sage::kBF16 && SAGE_E4M3 == sage::kE4M3, "types");
+
+}  // namespace
+
+// ------------------------------------------------------------------ lookup
+SAGE_API size_t sage_embed_workspace_bytes(int T, int Q, int d) {
+  return embed_sizes_ok(T, Q, d) ? sage::embed_workspace_bytes(T, Q, d) : 0;
+}
+
+SAGE_API int sage_embed(const int32_t* tokens, int T, const void* table, int table_type, int V, int d, float scale,
+                        const int32_t* offsets, int Q, int mean, void* out, int out_type, void* workspace,
+                        size_t workspace_bytes, sage_stream_t stream) {
+  int st = check_embed_sizes("sage_embed", T, V, d, scale, offsets != nullptr, Q);
+  if (st != SAGE_OK) return st;
+  if (!is_row_type(table_type)) return fail(SAGE_EINVAL, "sage_embed: table_type=%d is not SAGE_F32 or SAGE_BF16", table_type);
+  if (!is_row_type(out_type)) return fail(SAGE_EINVAL, "sage_embed: out_type=%d is not SAGE_F32 or SAGE_BF16", out_type);
+  if (mean && !offsets) return fail(SAGE_EINVAL, "sage_embed: a mean needs offsets");
+  const int rows = offsets ? Q : T;
+  if (rows == 0) return ok();
+  if ((st = check_pointers("sage_embed", {{tokens, "tokens", T == 0}, {table, "table", false}, {offsets, "offsets", true},
+                                          {out, "out", false}})) != SAGE_OK)
+    return st;
+  if (overlap(table, (size_t)V * d * type_bytes(table_type), out, (size_t)rows * d * type_bytes(out_type)))
+    return fail(SAGE_EINVAL, "sage_embed: out overlaps the table");
+  if ((st = check_workspace("sage_embed", workspace, workspace_bytes,
+                            offsets ? sage::embed_workspace_bytes(T, Q, d) : 0)) != SAGE_OK)
+    return st;
+  if ((st = check_device()) != SAGE_OK) return st;
+  return hip_status(sage::launch_embed(tokens, T, table, (sage::Type)table_type, V, d, scale,
+                                       sage::Prompts{offsets, offsets ? Q : 0, mean != 0}, out, (sage::Type)out_type,
+                                       workspace, (hipStream_t)stream),
+                    "embed launch");
+}
+
+SAGE_API size_t sage_embed_grad_workspace_bytes(int T, int Q, int V, int d) {
+  return embed_sizes_ok(T, Q, d) && V >= 1 && V <= kMaxRows ? sage::embed_grad_workspace_bytes(T, Q, V, d) : 0;
+}
+
+SAGE_API int sage_embed_grad(const int32_t* tokens, int T, const void* grad, int grad_type, int V, int d, float scale,
+                             const int32_t* offsets, int Q, int mean, const float* add, float* out, void* workspace,
+                             size_t workspace_bytes, sage_stream_t stream) {
+  int st = check_embed_sizes("sage_embed_grad", T, V, d, scale, offsets != nullptr, Q);
+  if (st != SAGE_OK) return st;
+  if (!is_row_type(grad_type)) return fail(SAGE_EINVAL, "sage_embed_grad: grad_type=%d is not SAGE_F32 or SAGE_BF16", grad_type);
+  if (mean && !offsets) return fail(SAGE_EINVAL, "sage_embed_grad: a mean needs offsets");
+  if (offsets && Q == 0) T = 0;                          // no prompt, so no token is in one
+  if ((st = check_pointers("sage_embed_grad", {{tokens, "tokens", T == 0}, {grad, "grad", T == 0}, {offsets, "offsets", true},
+                                               {add, "add", true}, {out, "out", false}})) != SAGE_OK)
+    return st;
+  const size_t out_bytes = (size_t)V * d * sizeof(float);
+  if (overlap(grad, (size_t)(offsets ? Q : T) * d * type_bytes(grad_type), out, out_bytes))
+    return fail(SAGE_EINVAL, "sage_embed_grad: out overlaps grad");
+  if (add != out && overlap(add, out_bytes, out, out_bytes))
+    return fail(SAGE_EINVAL, "sage_embed_grad: out overlaps add in part");
+  if ((st = check_workspace("sage_embed_grad", workspace, workspace_bytes,
+                            sage::embed_grad_workspace_bytes(T, offsets ? Q : 0, V, d))) != SAGE_OK)
+    return st;
+  if ((st = check_device()) != SAGE_OK) return st;
+  return hip_status(sage::launch_embed_grad(tokens, T, grad, (sage::Type)grad_type, V, d, scale,
+                                            sage::Prompts{offsets, offsets ? Q : 0, mean != 0}, add, out, workspace,
+                                            (hipStream_t)stream),
+                    "embed_grad launch");
+}
+
+// -------------------------------------------------------------------- norm
+SAGE_API int sage_rms_norm(const void* x, const void* residual, int type, int M, int d, const float* gain, float eps,
+                           void* total, void* out, int out_type, float* scales, sage_stream_t stream) {
+  int st = check_norm_sizes("sage_rms_norm", type, M, d, eps);
+  if (st != SAGE_OK) return st;
+  if (!is_row_type(out_type) && out_type != SAGE_E4M3)
+    return fail(SAGE_EINVAL, "sage_rms_norm: out_type=%d is not a SAGE_* type", out_type);
+  if (M == 0) return ok();
+  if ((st = check_pointers("sage_rms_norm", {{x, "x", false}, {residual, "residual", true}, {gain, "gain", false},
+                                             {total, "total", true}, {out, "out", false},
+                                             {scales, "scales", out_type != SAGE_E4M3}})) != SAGE_OK)
+    return st;
+  const size_t in_bytes = (size_t)M * d * type_bytes(type);
+  const size_t cols = out_type == SAGE_E4M3 ? (size_t)sage::pad16(d) : (size_t)d;
+  const size_t out_bytes = (size_t)M * cols * type_bytes(out_type);
+  if (overlap(x, in_bytes, out, out_bytes) || overlap(residual, in_bytes, out, out_bytes) ||
+      overlap(total, in_bytes, out, out_bytes))
+    return fail(SAGE_EINVAL, "sage_rms_norm: out overlaps x, residual or total");
+  if ((total != x && overlap(x, in_bytes, total, in_bytes)) ||
+      (total != residual && overlap(residual, in_bytes, total, in_bytes)))
+    return fail(SAGE_EINVAL, "sage_rms_norm: total overlaps x or residual in part");
+  if ((st = check_device()) != SAGE_OK) return st;
+  return hip_status(sage::launch_rms_norm(x, residual, (sage::Type)type, M, d, gain, eps, total, out,
+                                          (sage::Type)out_type, scales, (hipStream_t)stream),
+                    "rms_norm launch");
+}
+
+SAGE_API size_t sage_rms_norm_grad_workspace_bytes(int M, int d) {
+  return M > 0 && M <= kMaxRows && d >= 1 && d <= SAGE_MAX_NORM_COLS ? sage::rms_norm_grad_workspace_bytes(M, d) : 0;
+}
+
+SAGE_API int sage_rms_norm_grad(const void* grad, const void* total, int type, int M, int d, const float* gain, float eps,
+                                const void* grad_total, void* grad_x, float* grad_gain, void* workspace,
+                                size_t workspace_bytes, sage_stream_t stream) {
+  int st = check_norm_sizes("sage_rms_norm_grad", type, M, d, eps);
+  if (st != SAGE_OK) return st;
+  if ((st = check_pointers("sage_rms_norm_grad", {{grad, "grad", M == 0}, {total, "total", M == 0}, {gain, "gain", M == 0},
+                                                  {grad_total, "grad_total", true}, {grad_x, "grad_x", M == 0},
+                                                  {grad_gain, "grad_gain", false}})) != SAGE_OK)
+    return st;
+  const size_t bytes = (size_t)M * d * type_bytes(type);
+  const void* in[] = {grad, total, grad_total};
+  for (const void* p : in)
+    if (p != grad_x && overlap(p, bytes, grad_x, bytes))
+      return fail(SAGE_EINVAL, "sage_rms_norm_grad: grad_x overlaps an input in part");
+  if ((st = check_workspace("sage_rms_norm_grad", workspace, workspace_bytes,
+                            M > 0 ? sage::rms_norm_grad_workspace_bytes(M, d) : 0)) != SAGE_OK)
+    return st;
+  if ((st = check_device()) != SAGE_OK) return st;
+  return hip_status(sage::launch_rms_norm_grad(grad, total, (sage::Type)type, M, d, gain, eps, grad_total, grad_x,
+                                               grad_gain, workspace, (hipStream_t)stream),
+                    "rms_norm_grad launch");
+}
+
+// ------------------------------------------------------------ 8-bit blocks
+SAGE_API int sage_quantize(const void* x, int type, int M, int K, int block, int transpose, uint8_t* q, float* scales,
+                           sage_stream_t stream) {
+  if (!is_row_type(type)) return fail(SAGE_EINVAL, "sage_quantize: type=%d is not SAGE_F32 or SAGE_BF16", type);
+  if (block != SAGE_BLOCK_ROW && block != SAGE_BLOCK_SQUARE)
+    return fail(SAGE_EINVAL, "sage_quantize: block=%d is not a SAGE_BLOCK_* value", block);
+  if (M < 0 || M > kMaxRows) return fail(SAGE_EINVAL, "sage_quantize: M=%d outside [0, 2^30]", M);
+  if (K < 0 || K > kMaxRows) return fail(SAGE_EINVAL, "sage_quantize: K=%d outside [0, 2^30]", K);
+  if ((long long)M * sage::ceil_div(K, sage::kBlock) >= (1LL << 28))
+    return fail(SAGE_EINVAL, "sage_quantize: M * ceil(K / 128) not below 2^28");
+  if (M == 0 || K == 0) return ok();
+  int st;
+  if ((st = check_pointers("sage_quantize", {{x, "x", false}, {q, "q", false}, {scales, "scales", false}})) != SAGE_OK)
+    return st;
+  const size_t q_bytes = transpose ? (size_t)K * sage::pad16(M) : (size_t)M * sage::pad16(K);
+  if (overlap(x, (size_t)M * K * type_bytes(type), q, q_bytes)) return fail(SAGE_EINVAL, "sage_quantize: q overlaps x");
+  if ((st = check_device()) != SAGE_OK) return st;
+  return hip_status(sage::launch_quantize(x, (sage::Type)type, M, K, block == SAGE_BLOCK_SQUARE, transpose != 0, q,
+                                          scales, (hipStream_t)stream),
+                    "quantize launch");
+}
+
+// ------------------------------------------------------------------ product
+namespace {
+int check_matmul_sizes(int M, int N, int K) {
+  if (M < 0 || M > kMaxRows) return fail(SAGE_EINVAL, "sage_matmul_fp8: M=%d outside [0, 2^30]", M);
+  if (N < 0 || N > kMaxRows) return fail(SAGE_EINVAL, "sage_matmul_fp8: N=%d outside [0, 2^30]", N);
+  if (K < 16 || K > kMaxCols || K % 16 != 0)
+    return fail(SAGE_EINVAL, "sage_matmul_fp8: K=%d is not a multiple of 16 in [16, 2^20]", K);
+  if ((long long)sage::ceil_div(M, 128) * sage::ceil_div(N, 128) >= (1LL << 22))
+    return fail(SAGE_EINVAL, "sage_matmul_fp8: M=%d x N=%d is not below 2^22 tiles of 128 x 128", M, N);
+  return SAGE_OK;
+}
+}  // namespace
+
+SAGE_API size_t sage_matmul_fp8_workspace_bytes(int M, int N, int K) {
+  if (M < 1 || M > kMaxRows || N < 1 || N > kMaxRows || K < 16 || K > kMaxCols || K % 16 != 0 ||
+      (long long)sage::ceil_div(M, 128) * sage::ceil_div(N, 128) >= (1LL << 22))
+    return 0;
+  return sage::matmul_fp8_workspace_bytes(M, N, K);
+}
+
+SAGE_API int sage_matmul_fp8(const uint8_t* a, const float* a_scales, int M, const uint8_t* b, const float* b_scales,
+                             int b_block, int N, int K, const float* bias, int relu, int fast_accum, void* out,
+                             int out_type, void* workspace, size_t workspace_bytes, sage_stream_t stream) {
+  int st = check_matmul_sizes(M, N, K);
+  if (st != SAGE_OK) return st;
+  if (b_block != SAGE_BLOCK_ROW && b_block != SAGE_BLOCK_SQUARE)
+    return fail(SAGE_EINVAL, "sage_matmul_fp8: b_block=%d is not a SAGE_BLOCK_* value", b_block);
+  if (!is_row_type(out_type)) return fail(SAGE_EINVAL, "sage_matmul_fp8: out_type=%d is not SAGE_F32 or SAGE_BF16", out_type);
+  if (M == 0 || N == 0) return ok();
+  if ((st = check_pointers("sage_matmul_fp8", {{a, "a", false}, {a_scales, "a_scales", false}, {b, "b", false},
+                                               {b_scales, "b_scales", false}, {bias, "bias", true}, {out, "out", false}})) !=
+      SAGE_OK)
+    return st;
+  const size_t out_bytes = (size_t)M * N * type_bytes(out_type);
+  if (overlap(a, (size_t)M * K, out, out_bytes) || overlap(b, (size_t)N * K, out, out_bytes))
+    return fail(SAGE_EINVAL, "sage_matmul_fp8: out overlaps an operand");
+  if ((st = check_workspace("sage_matmul_fp8", workspace, workspace_bytes,
+                            sage::matmul_fp8_workspace_bytes(M, N, K))) != SAGE_OK)
+    return st;
+  if ((st = check_device()) != SAGE_OK) return st;
+  const sage::Fp8Product p{a, b, a_scales, b_scales, b_block == SAGE_BLOCK_SQUARE, M, N, K,
+                           bias, relu != 0, fast_accum != 0, out, (sage::Type)out_type};
+  return hip_status(sage::launch_matmul_fp8(p, workspace, (hipStream_t)stream), "matmul_fp8 launch");
+}

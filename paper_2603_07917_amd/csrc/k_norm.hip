@@ -1,0 +1,440 @@
+// Root-mean-square norm with the residual's addition, its backward pass, and
+// 8-bit blocks with scales.
+//
+// Norm. Per row of d columns: s = x + r, total = s rounded to the input's
+// type, w = (mean(s^2) + eps)^(-1/2), n = s w g. The statistics and n come
+// from the unrounded fp32 sum. Backward, with s read back from `total`:
+//   u = g dy, grad_x = w u - s w^3 / d sum(u s) + grad_total,
+//   grad_gain = sum over rows of dy s w.
+// Both read a row once into registers (8 columns a lane and step) and are
+// bound by the memory's rate.
+#include "sage_encode.hpp"
+#include "sage_internal.hpp"
+
+namespace sage {
+namespace {
+
+constexpr int kCols = 8;                                 // consecutive columns of a lane in one step
+
+constexpr int kNormGrid = 1 << 20;                       // workgroups at most; rows past them in turns
+
+// A row takes L lanes of a wave (L = 16, 32, 64), or W whole waves (L = 64),
+// in S steps of 8 columns per lane: L * W * S * 8 >= d. A block of 128
+// columns is 16 neighbouring lanes, so its amax needs no LDS.
+template <int W>
+__device__ __forceinline__ float row_sum(float x, float* lds, int w) {
+  if constexpr (W > 1) {
+    if (lane_id() == 0) lds[w] = x;
+    __syncthreads();
+    x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) x += lds[i];
+  }
+  return x;
+}
+
+template <class T, int kOut, int L, int W, int S, bool kAligned>
+__global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_kernel(
+    const T* x, const T* residual, int M, int d, const float* __restrict__ gain, float eps, T* total, void* out,
+    float* __restrict__ scales) {
+  constexpr int kThreads = W > 4 ? 64 * W : 256;
+  constexpr int kRows = kThreads / (L * W);              // rows per workgroup
+  __shared__ float lds[2][kRows == 1 ? W : 1];
+  const int in_row = threadIdx.x % (L * W);
+  int turn = 0;
+  for (int row = blockIdx.x * kRows + (int)threadIdx.x / (L * W); row < M; row += gridDim.x * kRows, turn ^= 1) {
+  const long long base = (long long)row * d;
+
+  float s[S][kCols];
+  float sq = 0.0f;
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    const int col = (i * L * W + in_row) * kCols;
+    load_row<T, kCols, kAligned>(s[i], x + base, col, d);
+    if (residual) {
+      float r[kCols];
+      load_row<T, kCols, kAligned>(r, residual + base, col, d);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) s[i][j] += r[j];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    if (total) store_row<T, kCols, kAligned>(s[i], total + base, (i * L * W + in_row) * kCols, d);
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) sq = fmaf(s[i][j], s[i][j], sq);
+  }
+  sq = row_sum<W>(group_sum_f32<L>(sq), lds[turn], in_row / 64);
+  const float w = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(sq, (float)d) + eps));
+
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    const int col = (i * L * W + in_row) * kCols;
+    float g[kCols];
+    load_row<float, kCols, kAligned>(g, gain, col, d);
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) s[i][j] = s[i][j] * w * g[j];
+    if constexpr (kOut == kE4M3) {
+      float amax = 0.0f;
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) amax = fmaxf(amax, finite_mag(s[i][j]));
+      amax = group_max_f32<16>(amax);
+      const float scale = block_scale(amax), inv = __fdiv_rn(1.0f, scale);
+      const int dp = (d + 15) & ~15;
+      if (col < dp) {
+        uint2 q;
+        q.x = e4m3x4(s[i][0] * inv, s[i][1] * inv, s[i][2] * inv, s[i][3] * inv);
+        q.y = e4m3x4(s[i][4] * inv, s[i][5] * inv, s[i][6] * inv, s[i][7] * inv);
+        if (col >= d) q = make_uint2(0u, 0u);            // the padding, also of a row of NaN
+        else if (!kAligned && col + kCols > d) {
+          const uint64_t keep = ~0ull >> (8 * (col + kCols - d));
+          q.x &= (uint32_t)keep;
+          q.y &= (uint32_t)(keep >> 32);
+        }
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out) + (long long)row * dp + col) = q;
+        if (col % kBlock == 0) scales[(long long)(col / kBlock) * M + row] = scale;
+      }
+    } else if constexpr (kOut == kBF16) {
+      store_row<bf16, kCols, kAligned>(s[i], static_cast<bf16*>(out) + base, col, d);
+    } else {
+      store_row<float, kCols, kAligned>(s[i], static_cast<float*>(out) + base, col, d);
+    }
+  }
+  }
+}
+
+template <class T, int kOut, bool kAligned>
+hipError_t norm_by_width(const T* x, const T* residual, int M, int d, const float* gain, float eps, T* total, void* out,
+                         float* scales, hipStream_t stream) {
+  LaunchScope scope("rms_norm_kernel", stream);
+#define SAGE_NORM(L, W, S)                                                                              \
+  rms_norm_kernel<T, kOut, L, W, S, kAligned>                                                           \
+      <<<min(kNormGrid, ceil_div(M, (W > 4 ? 64 * W : 256) / (L * W))), W > 4 ? 64 * W : 256, 0, stream>>>(             \
+          x, residual, M, d, gain, eps, total, out, scales)
+  if (d <= 128) SAGE_NORM(16, 1, 1);
+  else if (d <= 256) SAGE_NORM(32, 1, 1);
+  else if (d <= 512) SAGE_NORM(64, 1, 1);
+  else if (d <= 1024) SAGE_NORM(64, 1, 2);
+  else if (d <= 2048) SAGE_NORM(64, 1, 4);
+  else if (d <= 4096) SAGE_NORM(64, 4, 2);
+  else if (d <= 8192) SAGE_NORM(64, 4, 4);
+  else if (d <= 16384) SAGE_NORM(64, 8, 4);
+  else SAGE_NORM(64, 16, 4);
+#undef SAGE_NORM
+  return hipGetLastError();
+}
+
+template <class T, bool kAligned>
+hipError_t norm_by_out(const void* x, const void* residual, int M, int d, const float* gain, float eps, void* total,
+                       void* out, Type out_type, float* scales, hipStream_t stream) {
+  const T *xs = static_cast<const T*>(x), *rs = static_cast<const T*>(residual);
+  T* ts = static_cast<T*>(total);
+  if (out_type == kE4M3) return norm_by_width<T, kE4M3, kAligned>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
+  if (out_type == kBF16) return norm_by_width<T, kBF16, kAligned>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
+  return norm_by_width<T, kF32, kAligned>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
+}
+
+// ------------------------------------------------------------- backward pass
+// A workgroup takes kGroup = 4 / W rows at a time and every gridDim.x-th such
+// group, and keeps its columns' sums of dy s w in registers; each workgroup's
+// sums go to a row of `part`, which norm_gain_kernel adds in a fixed order.
+constexpr int kGradGroups = 1024;                        // at most this many rows of partial sums
+
+template <class T, int L, int W, int S, bool kAligned>
+__global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_grad_kernel(
+    const T* grad, const T* total, int M, int d, const float* __restrict__ gain, float eps, const T* grad_total,
+    T* grad_x, float* __restrict__ part) {
+  constexpr int kThreads = W > 4 ? 64 * W : 256;
+  constexpr int kRows = kThreads / (L * W);
+  __shared__ float lds[2][kRows == 1 ? 2 * W : 1];
+  __shared__ float sums[kRows == 1 ? 1 : 256 * S * kCols];
+  const int in_row = threadIdx.x % (L * W);
+  const int slot = (int)threadIdx.x / (L * W);
+  float dg[S][kCols] = {};
+  int turn = 0;
+  for (int first = blockIdx.x * kRows; first < M; first += gridDim.x * kRows, turn ^= 1) {
+    const int row = first + slot;
+    if (kRows > 1 && row >= M) continue;
+    const long long base = (long long)row * d;
+    float s[S][kCols], dy[S][kCols];
+    float sq = 0.0f, us = 0.0f;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int col = (i * L * W + in_row) * kCols;
+      load_row<T, kCols, kAligned>(s[i], total + base, col, d);
+      load_row<T, kCols, kAligned>(dy[i], grad + base, col, d);
+    }
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      float g[kCols];
+      load_row<float, kCols, kAligned>(g, gain, (i * L * W + in_row) * kCols, d);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) {
+        sq = fmaf(s[i][j], s[i][j], sq);
+        us = fmaf(dy[i][j] * g[j], s[i][j], us);
+      }
+    }
+    sq = group_sum_f32<L>(sq);
+    us = group_sum_f32<L>(us);
+    if constexpr (W > 1) {                               // two buffers in turn: one barrier a row
+      if (lane_id() == 0) lds[turn][2 * (in_row / 64)] = sq, lds[turn][2 * (in_row / 64) + 1] = us;
+      __syncthreads();
+      sq = us = 0.0f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) sq += lds[turn][2 * i], us += lds[turn][2 * i + 1];
+    }
+    const float w = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(sq, (float)d) + eps));
+    const float c = w * w * w * __fdiv_rn(us, (float)d);
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int col = (i * L * W + in_row) * kCols;
+      float g[kCols], o[kCols];
+      load_row<float, kCols, kAligned>(g, gain, col, d);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) {
+        dg[i][j] = fmaf(dy[i][j] * s[i][j], w, dg[i][j]);
+        o[j] = fmaf(dy[i][j] * g[j], w, -s[i][j] * c);
+      }
+      if (grad_total) {
+        float t[kCols];
+        load_row<T, kCols, kAligned>(t, grad_total + base, col, d);
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) o[j] += t[j];
+      }
+      store_row<T, kCols, kAligned>(o, grad_x + base, col, d);
+    }
+  }
+  float* mine = part + (long long)blockIdx.x * d;
+  if constexpr (kRows == 1) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) store_row<float, kCols, kAligned>(dg[i], mine, (i * L * W + in_row) * kCols, d);
+  } else {
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) sums[((i * kCols + j) * kRows + slot) * L * W + in_row] = dg[i][j];
+    __syncthreads();
+    // Column (i L W + in_row) kCols + j, by any thread.
+    for (int k = threadIdx.x; k < L * W * S * kCols; k += kThreads) {
+      const int e = k / (L * W), r = k % (L * W), col = ((e / kCols) * L * W + r) * kCols + e % kCols;
+      float t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) t += sums[(e * kRows + i) * L * W + r];
+      if (col < d) mine[col] = t;
+    }
+  }
+}
+
+// grad_gain[c] = sum of part[0..rows)[c]: 64 columns a workgroup, 16 lanes of rows.
+__global__ void __launch_bounds__(1024) norm_gain_kernel(const float* __restrict__ part, int rows, int d,
+                                                         float* __restrict__ grad_gain) {
+  __shared__ float sums[16][64];
+  const int c = threadIdx.x % 64, g = threadIdx.x / 64, col = blockIdx.x * 64 + c;
+  float t = 0.0f;
+  if (col < d)
+    for (int r = g; r < rows; r += 16) t += part[(long long)r * d + col];
+  sums[g][c] = t;
+  __syncthreads();
+  if (g == 0 && col < d) {
+    t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += sums[i][c];
+    grad_gain[col] = t;
+  }
+}
+
+int norm_rows_per_group(int d) { return d <= 128 ? 16 : d <= 256 ? 8 : d <= 2048 ? 4 : 1; }
+int norm_grad_groups(int M, int d) { return min(kGradGroups, ceil_div(M, norm_rows_per_group(d))); }
+
+template <class T, bool kAligned>
+hipError_t norm_grad_by_width(const void* grad, const void* total, int M, int d, const float* gain, float eps,
+                              const void* grad_total, void* grad_x, float* grad_gain, float* part,
+                              hipStream_t stream) {
+  const int groups = norm_grad_groups(M, d);
+  if (groups > 0) {
+    LaunchScope scope("rms_norm_grad_kernel", stream);
+#define SAGE_NORM_GRAD(L, W, S)                                                                       \
+  rms_norm_grad_kernel<T, L, W, S, kAligned><<<groups, W > 4 ? 64 * W : 256, 0, stream>>>(            \
+      static_cast<const T*>(grad), static_cast<const T*>(total), M, d, gain, eps,                     \
+      static_cast<const T*>(grad_total), static_cast<T*>(grad_x), part)
+    if (d <= 128) SAGE_NORM_GRAD(16, 1, 1);
+    else if (d <= 256) SAGE_NORM_GRAD(32, 1, 1);
+    else if (d <= 512) SAGE_NORM_GRAD(64, 1, 1);
+    else if (d <= 1024) SAGE_NORM_GRAD(64, 1, 2);
+    else if (d <= 2048) SAGE_NORM_GRAD(64, 1, 4);
+    else if (d <= 4096) SAGE_NORM_GRAD(64, 4, 2);
+    else if (d <= 8192) SAGE_NORM_GRAD(64, 4, 4);
+    else if (d <= 16384) SAGE_NORM_GRAD(64, 8, 4);
+    else SAGE_NORM_GRAD(64, 16, 4);
+#undef SAGE_NORM_GRAD
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  LaunchScope scope("norm_gain_kernel", stream);
+  norm_gain_kernel<<<ceil_div(d, 64), 1024, 0, stream>>>(part, groups, d, grad_gain);
+  return hipGetLastError();
+}
+
+// -------------------------------------------------------------- 8-bit blocks
+// 1 x 128 blocks, as they lie: 16 lanes a block, 8 values each.
+template <class T, bool kAligned>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict__ x, int M, int K, int kb,
+                                                            uint8_t* __restrict__ q, float* __restrict__ scales) {
+  const long long blk = ((long long)blockIdx.x * 256 + threadIdx.x) / 16;
+  if (blk >= (long long)M * kb) return;
+  const int row = (int)(blk / kb), b = (int)(blk % kb), in_block = threadIdx.x % 16;
+  const int col = b * kBlock + in_block * kCols, kp = (K + 15) & ~15;
+  float v[kCols];
+  load_row<T, kCols, kAligned>(v, x + (long long)row * K, col, K);
+  float amax = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kCols; ++j) amax = fmaxf(amax, finite_mag(v[j]));
+  const float scale = block_scale(group_max_f32<16>(amax)), inv = __fdiv_rn(1.0f, scale);
+  if (col < kp)
+    *reinterpret_cast<uint2*>(q + (long long)row * kp + col) =
+        make_uint2(e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                   e4m3x4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+  if (in_block == 0) scales[(long long)b * M + row] = scale;
+}
+
+// A tile of 128 rows x 128 columns of x: one scale for all of it (kSquare), or
+// one per column (the rows of the transpose). Thread (t / 16, t % 16) holds 8
+// rows x 8 columns. Transposed tiles pass through LDS as bytes, 8 rows of one
+// column at a time, and leave as whole 128-byte lines.
+template <class T, bool kSquare, bool kTranspose, bool kAligned>
+__global__ void __launch_bounds__(256) quantize_tile_kernel(const T* __restrict__ x, int M, int K, int kb, int mb,
+                                                            uint8_t* __restrict__ q, float* __restrict__ scales) {
+  constexpr int kPitch = kBlock + 8;                     // bytes between the tile's columns in LDS
+  __shared__ float red[4][kSquare ? 1 : kBlock];
+  __shared__ __attribute__((aligned(16))) uint8_t tile[kTranspose ? kBlock * kPitch : 16];
+  const int w = threadIdx.x / 64, cg = threadIdx.x % 16, rg = threadIdx.x / 16;
+  const int by = blockIdx.x / kb, bx = blockIdx.x % kb;
+  const int r0 = by * kBlock, c0 = bx * kBlock, col = c0 + cg * kCols;
+  float v[8][kCols];
+  float top[kCols] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + rg * 8 + i;
+    load_row<T, kCols, kAligned>(v[i], x + (long long)r * K, r < M ? col : K, K);
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) top[j] = fmaxf(top[j], finite_mag(v[i][j]));
+  }
+  float inv[kCols];
+  if constexpr (kSquare) {
+    float m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) m = fmaxf(m, top[j]);
+    m = group_max_f32<64>(m);
+    if (lane_id() == 0) red[w][0] = m;
+    __syncthreads();
+    const float scale = block_scale(fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0])));
+    if (threadIdx.x == 0) {
+      if constexpr (kTranspose) scales[(long long)by * kb + bx] = scale;
+      else scales[(long long)bx * mb + by] = scale;
+    }
+    const float one = __fdiv_rn(1.0f, scale);
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) inv[j] = one;
+  } else {
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) {
+      float m = top[j];
+      m = fmaxf(m, __uint_as_float(xor_lane_u32<16>(__float_as_uint(m))));
+      m = fmaxf(m, __uint_as_float(xor_lane_u32<32>(__float_as_uint(m))));
+      if ((threadIdx.x & 48) == 0) red[w][cg * kCols + j] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) {
+      const int c = cg * kCols + j;
+      const float scale = block_scale(fmaxf(fmaxf(red[0][c], red[1][c]), fmaxf(red[2][c], red[3][c])));
+      if (rg == 0 && c0 + c < K) scales[(long long)by * K + c0 + c] = scale;
+      inv[j] = __fdiv_rn(1.0f, scale);
+    }
+  }
+  if constexpr (!kTranspose) {
+    const int kp = (K + 15) & ~15;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + rg * 8 + i;
+      if (r < M && col < kp)
+        *reinterpret_cast<uint2*>(q + (long long)r * kp + col) =
+            make_uint2(e4m3x4(v[i][0] * inv[0], v[i][1] * inv[1], v[i][2] * inv[2], v[i][3] * inv[3]),
+                       e4m3x4(v[i][4] * inv[4], v[i][5] * inv[5], v[i][6] * inv[6], v[i][7] * inv[7]));
+    }
+  } else {
+    const int mp = (M + 15) & ~15;
+#pragma unroll
+    for (int j = 0; j < kCols; ++j)
+      *reinterpret_cast<uint2*>(tile + (cg * kCols + j) * kPitch + rg * 8) =
+          make_uint2(e4m3x4(v[0][j] * inv[j], v[1][j] * inv[j], v[2][j] * inv[j], v[3][j] * inv[j]),
+                     e4m3x4(v[4][j] * inv[j], v[5][j] * inv[j], v[6][j] * inv[j], v[7][j] * inv[j]));
+    __syncthreads();
+    // 8 lanes write 16 bytes each of one column: a row of the transpose.
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = i * 32 + threadIdx.x / 8, m = (threadIdx.x % 8) * 16;
+      if (c0 + c < K && r0 + m < mp) {
+        const uint2* p = reinterpret_cast<const uint2*>(tile + c * kPitch + m);
+        const uint2 a = p[0], b = p[1];
+        *reinterpret_cast<uint4*>(q + (long long)(c0 + c) * mp + r0 + m) = make_uint4(a.x, a.y, b.x, b.y);
+      }
+    }
+  }
+}
+
+template <class T, bool kAligned>
+hipError_t quantize_by_block(const void* xv, int M, int K, bool square, bool transpose, uint8_t* q, float* scales,
+                             hipStream_t stream) {
+  const T* x = static_cast<const T*>(xv);
+  if (!square && !transpose) {
+    LaunchScope scope("quantize_rows_kernel", stream);
+    const int kb = ceil_div(K, kBlock);
+    const long long threads = (long long)M * kb * 16;
+    quantize_rows_kernel<T, kAligned><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(x, M, K, kb, q, scales);
+    return hipGetLastError();
+  }
+  LaunchScope scope("quantize_tile_kernel", stream);
+  const int kb = ceil_div(K, kBlock), mb = ceil_div(M, kBlock);
+  const unsigned grid = (unsigned)kb * (unsigned)mb;
+  if (square && transpose) quantize_tile_kernel<T, true, true, kAligned><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
+  else if (square) quantize_tile_kernel<T, true, false, kAligned><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
+  else quantize_tile_kernel<T, false, true, kAligned><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const void* x, const void* residual, Type type, int M, int d, const float* gain, float eps,
+                           void* total, void* out, Type out_type, float* scales, hipStream_t stream) {
+  if (d % 8 == 0)
+    return type == kBF16 ? norm_by_out<bf16, true>(x, residual, M, d, gain, eps, total, out, out_type, scales, stream)
+                         : norm_by_out<float, true>(x, residual, M, d, gain, eps, total, out, out_type, scales, stream);
+  return type == kBF16 ? norm_by_out<bf16, false>(x, residual, M, d, gain, eps, total, out, out_type, scales, stream)
+                       : norm_by_out<float, false>(x, residual, M, d, gain, eps, total, out, out_type, scales, stream);
+}
+
+size_t rms_norm_grad_workspace_bytes(int M, int d) { return (size_t)norm_grad_groups(M, d) * d * sizeof(float); }
+
+hipError_t launch_rms_norm_grad(const void* grad, const void* total, Type type, int M, int d, const float* gain,
+                                float eps, const void* grad_total, void* grad_x, float* grad_gain, void* ws,
+                                hipStream_t stream) {
+  float* part = static_cast<float*>(ws);
+  const bool aligned = d % 8 == 0;
+  if (type == kBF16)
+    return aligned ? norm_grad_by_width<bf16, true>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream)
+                   : norm_grad_by_width<bf16, false>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream);
+  return aligned ? norm_grad_by_width<float, true>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream)
+                 : norm_grad_by_width<float, false>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream);
+}
+
+hipError_t launch_quantize(const void* x, Type type, int M, int K, bool square, bool transpose, uint8_t* q,
+                           float* scales, hipStream_t stream) {
+  if (K % 8 == 0)
+    return type == kBF16 ? quantize_by_block<bf16, true>(x, M, K, square, transpose, q, scales, stream)
+                         : quantize_by_block<float, true>(x, M, K, square, transpose, q, scales, stream);
+  return type == kBF16 ? quantize_by_block<bf16, false>(x, M, K, square, transpose, q, scales, stream)
+                       : quantize_by_block<float, false>(x, M, K, square, transpose, q, scales, stream);
+}
+
+}  // namespace sage

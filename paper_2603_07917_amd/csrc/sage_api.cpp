@@ -12,16 +12,15 @@
 #include <vector>
 
 #include "sage.h"
+#include "sage_api.hpp"
 #include "sage_internal.hpp"
 
-#define SAGE_API extern "C" __attribute__((visibility("default")))
-
 namespace {
-
 thread_local std::string g_last_error;
 thread_local sage_timer* g_timer = nullptr;
+}  // namespace
 
-int fail(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace sage {
 int fail(int status, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -65,7 +64,15 @@ int hip_status(hipError_t e, const char* what) {
   if (e != hipSuccess) return fail(SAGE_EHIP, "%s: %s", what, hipGetErrorString(e));
   return ok();
 }
+}  // namespace sage
 
+using sage::aligned16;
+using sage::check_device;
+using sage::fail;
+using sage::hip_status;
+using sage::ok;
+
+namespace {
 constexpr float kMinTau = 9.5367431640625e-07f;   // 2^-20
 
 int check_bins(const double* edges, int B) {

@@ -1,0 +1,174 @@
+// Internals shared by the prompt encoder's kernels (embedding lookup, norm,
+// 8-bit blocks, 8-bit product): element types, row vectors, launchers.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "sage_device.hpp"
+
+namespace sage {
+
+using bf16 = __bf16;
+enum Type { kF32 = 0, kBF16 = 1, kE4M3 = 2 };            // SAGE_F32, SAGE_BF16, SAGE_E4M3
+constexpr int kBlock = 128;                              // columns that share a scale
+constexpr float kE4M3Max = 448.0f;
+constexpr float kMinScale = 1.1754943508222875e-38f;     // 2^-126: its reciprocal is finite
+inline int ceil_div(int a, int b) { return a / b + (a % b != 0); }
+inline int pad16(int n) { return (n + 15) & ~15; }
+
+// ---------------------------------------------------------------------------
+// V consecutive elements of a row, as fp32. kAligned: row starts and d are
+// such that a whole vector can be loaded at once and is inside the row or
+// outside it; otherwise element by element. Columns from d on read as 0.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float from_bits_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float from_bits_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+
+template <class T, int V, bool kAligned>
+__device__ __forceinline__ void load_row(float (&v)[V], const T* row, int col, int d) {
+  if constexpr (kAligned) {
+    if (col < d) {
+      if constexpr (sizeof(T) == 2) {
+        static_assert(V % 8 == 0, "whole 16-byte pieces");
+#pragma unroll
+        for (int i = 0; i < V; i += 8) {
+          const uint4 u = *reinterpret_cast<const uint4*>(row + col + i);
+          v[i] = from_bits_lo(u.x), v[i + 1] = from_bits_hi(u.x);
+          v[i + 2] = from_bits_lo(u.y), v[i + 3] = from_bits_hi(u.y);
+          v[i + 4] = from_bits_lo(u.z), v[i + 5] = from_bits_hi(u.z);
+          v[i + 6] = from_bits_lo(u.w), v[i + 7] = from_bits_hi(u.w);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(row + col + i);
+          v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = 0.0f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = col + i < d ? (float)row[col + i] : 0.0f;
+  }
+}
+
+// Two fp32 values as bf16 bits (round to nearest even, NaN kept).
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  union { bf16 h[2]; uint32_t u; } p;
+  p.h[0] = (bf16)a;
+  p.h[1] = (bf16)b;
+  return p.u;
+}
+
+template <class T, int V, bool kAligned>
+__device__ __forceinline__ void store_row(const float (&v)[V], T* row, int col, int d) {
+  if constexpr (kAligned) {
+    if (col < d) {
+      if constexpr (sizeof(T) == 2) {
+        if constexpr (V == 4) {
+          *reinterpret_cast<uint2*>(row + col) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; i += 8)
+            *reinterpret_cast<uint4*>(row + col + i) =
+                make_uint4(bf16_pair(v[i], v[i + 1]), bf16_pair(v[i + 2], v[i + 3]), bf16_pair(v[i + 4], v[i + 5]),
+                           bf16_pair(v[i + 6], v[i + 7]));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4)
+          *reinterpret_cast<float4*>(row + col + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (col + i < d) row[col + i] = (T)v[i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit values. A block's scale is max(amax / 448, 2^-126) over its finite
+// values; a value is stored as x * (1 / scale), rounded to the nearest e4m3
+// (ties to even). What is not finite becomes NaN and leaves the rest of its
+// block alone.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float finite_mag(float x) {
+  const float a = fabsf(x);
+  return a <= 3.402823466e38f ? a : 0.0f;
+}
+__device__ __forceinline__ float block_scale(float amax) { return fmaxf(__fdiv_rn(amax, kE4M3Max), kMinScale); }
+// Four values (already divided by their scale) as e4m3 bytes.
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+  int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, u, true);
+}
+
+// Maximum and sum over groups of G consecutive lanes, in every lane of them.
+template <int G>
+__device__ __forceinline__ float group_max_f32(float x) {
+  x = fmaxf(x, __uint_as_float(xor_lane_u32<1>(__float_as_uint(x))));
+  x = fmaxf(x, __uint_as_float(xor_lane_u32<2>(__float_as_uint(x))));
+  x = fmaxf(x, __uint_as_float(xor_lane_u32<4>(__float_as_uint(x))));
+  x = fmaxf(x, __uint_as_float(xor_lane_u32<8>(__float_as_uint(x))));
+  if constexpr (G >= 32) x = fmaxf(x, __uint_as_float(xor_lane_u32<16>(__float_as_uint(x))));
+  if constexpr (G >= 64) x = fmaxf(x, __uint_as_float(xor_lane_u32<32>(__float_as_uint(x))));
+  return x;
+}
+template <int G>
+__device__ __forceinline__ float group_sum_f32(float x) {
+  x += __uint_as_float(xor_lane_u32<1>(__float_as_uint(x)));
+  x += __uint_as_float(xor_lane_u32<2>(__float_as_uint(x)));
+  x += __uint_as_float(xor_lane_u32<4>(__float_as_uint(x)));
+  x += __uint_as_float(xor_lane_u32<8>(__float_as_uint(x)));
+  if constexpr (G >= 32) x += __uint_as_float(xor_lane_u32<16>(__float_as_uint(x)));
+  if constexpr (G >= 64) x += __uint_as_float(xor_lane_u32<32>(__float_as_uint(x)));
+  return x;
+}
+
+// ------------------------------------------------------------------ launchers
+// Each enqueues kernels on `stream` and returns the launch's HIP status.
+
+// The prompts of a list of tokens: offsets [Q + 1] (clamped to [0, T] and read
+// as non-decreasing), or none (each token by itself).
+struct Prompts {
+  const int32_t* offsets;
+  int Q;
+  bool mean;
+};
+size_t embed_workspace_bytes(int T, int Q, int d);
+hipError_t launch_embed(const int32_t* tokens, int T, const void* table, Type table_type, int V, int d, float scale,
+                        Prompts p, void* out, Type out_type, void* ws, hipStream_t stream);
+size_t embed_grad_workspace_bytes(int T, int Q, int V, int d);
+hipError_t launch_embed_grad(const int32_t* tokens, int T, const void* grad, Type grad_type, int V, int d, float scale,
+                             Prompts p, const float* add, float* out, void* ws, hipStream_t stream);
+
+constexpr int kMaxNormCols = 32768;
+hipError_t launch_rms_norm(const void* x, const void* residual, Type type, int M, int d, const float* gain, float eps,
+                           void* total, void* out, Type out_type, float* scales, hipStream_t stream);
+size_t rms_norm_grad_workspace_bytes(int M, int d);
+hipError_t launch_rms_norm_grad(const void* grad, const void* total, Type type, int M, int d, const float* gain,
+                                float eps, const void* grad_total, void* grad_x, float* grad_gain, void* ws,
+                                hipStream_t stream);
+hipError_t launch_quantize(const void* x, Type type, int M, int K, bool square, bool transpose, uint8_t* q,
+                           float* scales, hipStream_t stream);
+
+struct Fp8Product {
+  const uint8_t *a, *b;
+  const float *a_scales, *b_scales;
+  bool b_square;             // one scale per 128 x 128 block of b, not per row and 128 columns
+  int M, N, K;
+  const float* bias;
+  bool relu;
+  bool fast;                 // 8-bit MFMA, whose sums of 8 products are not fp32
+  void* out;
+  Type out_type;
+};
+size_t matmul_fp8_workspace_bytes(int M, int N, int K);
+hipError_t launch_matmul_fp8(const Fp8Product& p, void* ws, hipStream_t stream);
+
+}  // namespace sage

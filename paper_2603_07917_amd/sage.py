@@ -64,6 +64,16 @@ def load_library():
         "sage_debug_theta_floor": (I, [F]),
         "sage_decide_workspace_bytes": (Z, [I, I, I, I, I, I]),
         "sage_decide": (I, [P, I, I, P, I, P, I, I, I, F, P, P, P, I, P, P, P, P, P, P, P, Z, S]),
+        "sage_embed_workspace_bytes": (Z, [I, I, I]),
+        "sage_embed": (I, [P, I, P, I, I, I, F, P, I, I, P, I, P, Z, S]),
+        "sage_embed_grad_workspace_bytes": (Z, [I, I, I, I]),
+        "sage_embed_grad": (I, [P, I, P, I, I, I, F, P, I, I, P, P, P, Z, S]),
+        "sage_rms_norm": (I, [P, P, I, I, I, P, F, P, P, I, P, S]),
+        "sage_rms_norm_grad_workspace_bytes": (Z, [I, I]),
+        "sage_rms_norm_grad": (I, [P, P, I, I, I, P, F, P, P, P, P, Z, S]),
+        "sage_quantize": (I, [P, I, I, I, I, I, P, P, S]),
+        "sage_matmul_fp8_workspace_bytes": (Z, [I, I, I]),
+        "sage_matmul_fp8": (I, [P, P, I, P, P, I, I, I, P, I, I, P, I, P, Z, S]),
         "sage_status_string": (ctypes.c_char_p, [I]),
         "sage_last_error": (ctypes.c_char_p, []),
         "sage_timer_create": (I, [I, ctypes.POINTER(P)]),
@@ -474,6 +484,204 @@ def debug_theta_floor(floor: float):
     """Test hook: raise the pre-pass threshold of later predict calls to at
     least `floor` (-inf: off), forcing queries onto the exact fallback."""
     _check(load_library().sage_debug_theta_floor(float(floor)))
+
+
+# ---------------------------------------------------- prompt encoder operators
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+BLOCKS = {"row": 0, "square": 1}
+_ROW_TYPES = (torch.float32, torch.bfloat16)
+
+
+def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A contiguous fp32 or bf16 matrix on the device (of `like`'s type and shape)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _ROW_TYPES:
+        raise SageError(f"{name} must be a float32 or bfloat16 tensor")
+    _dev(t, t.dtype if like is None else like.dtype, name, 2)
+    if like is not None and t.shape != like.shape:
+        raise SageError(f"{name} must be {tuple(like.shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _result(out: Optional[torch.Tensor], shape, dtype, device, name: str = "out") -> torch.Tensor:
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _dev(out, dtype, name, len(shape))
+    if tuple(out.shape) != tuple(shape):
+        raise SageError(f"{name} must be {tuple(shape)}, got {tuple(out.shape)}")
+    return out
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> Optional[torch.Tensor]:
+    if need == 0 or (workspace is not None and workspace.numel() * workspace.element_size() >= need):
+        return workspace
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def _size(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _prompts(offsets: Optional[torch.Tensor], mean: bool) -> int:
+    if offsets is None:
+        if mean:
+            raise SageError("a mean needs offsets")
+        return 0
+    _dev(offsets, torch.int32, "offsets", 1)
+    if offsets.shape[0] < 1:
+        raise SageError("offsets must have one entry more than there are prompts")
+    return offsets.shape[0] - 1
+
+
+def embed(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, offsets: Optional[torch.Tensor] = None,
+          mean: bool = False, dtype: Optional[torch.dtype] = None, workspace: Optional[torch.Tensor] = None,
+          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Embedding rows of `tokens`, scaled: [T, d]; with `offsets` [Q + 1] the
+    sum (or mean) over each prompt's tokens: [Q, d]. Ids outside the table are
+    no tokens. `dtype` (float32 or bfloat16) is the table's by default."""
+    _dev(tokens, torch.int32, "tokens", 1)
+    _rows(table, "table")
+    Q, T, (V, d) = _prompts(offsets, mean), tokens.shape[0], table.shape
+    dtype = dtype or (table.dtype if out is None else out.dtype)
+    if dtype not in _ROW_TYPES:
+        raise SageError("dtype must be float32 or bfloat16")
+    out = _result(out, (T if offsets is None else Q, d), dtype, table.device)
+    lib = load_library()
+    ws = _scratch(workspace, 0 if offsets is None else lib.sage_embed_workspace_bytes(T, Q, d), table.device)
+    _check(lib.sage_embed(_ptr(tokens), T, _ptr(table), TYPES[table.dtype], V, d, float(scale), _ptr(offsets), Q,
+                          int(bool(mean)), _ptr(out), TYPES[dtype], _ptr(ws), _size(ws), _stream()))
+    return out
+
+
+def embed_grad(tokens: torch.Tensor, grad: torch.Tensor, vocab: int, scale: float = 1.0,
+               offsets: Optional[torch.Tensor] = None, mean: bool = False, add: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient [vocab, d] (fp32) of `embed` with respect to its table, plus
+    `add`; with out=add the gradient is added in place."""
+    _dev(tokens, torch.int32, "tokens", 1)
+    _rows(grad, "grad")
+    Q, T, V = _prompts(offsets, mean), tokens.shape[0], int(vocab)
+    rows, d = grad.shape
+    if rows != (T if offsets is None else Q):
+        raise SageError("grad must have one row per token, or per prompt with offsets")
+    if add is not None:
+        _dev(add, torch.float32, "add", 2)
+        if tuple(add.shape) != (V, d):
+            raise SageError(f"add must be {(V, d)}, got {tuple(add.shape)}")
+    out = _result(out, (V, d), torch.float32, grad.device)
+    lib = load_library()
+    ws = _scratch(workspace, lib.sage_embed_grad_workspace_bytes(T, Q, V, d), grad.device)
+    _check(lib.sage_embed_grad(_ptr(tokens), T, _ptr(grad), TYPES[grad.dtype], V, d, float(scale), _ptr(offsets), Q,
+                               int(bool(mean)), _ptr(add), _ptr(out), _ptr(ws), _size(ws), _stream()))
+    return out
+
+
+def _scale_shape(rows: int, cols: int, block: str):
+    return (-(-cols // 128), rows if block == "row" else -(-rows // 128))
+
+
+def rms_norm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+             dtype: Optional[torch.dtype] = None, total: Optional[torch.Tensor] = None,
+             out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None):
+    """Root-mean-square norm of s = x + residual: (out, scales, total).
+
+    `dtype` is the output's (x's by default); torch.float8_e4m3fn gives an
+    8-bit matrix [M, d rounded up to 16] and its scales [ceil(d / 128), M],
+    else scales is None. total is s in x's type (None without a residual,
+    unless a buffer is given; it may be x or residual itself)."""
+    _rows(x, "x")
+    M, d = x.shape
+    _dev(gain, torch.float32, "gain", 1)
+    if gain.shape[0] != d:
+        raise SageError("gain must have one entry per column")
+    if residual is not None:
+        _rows(residual, "residual", x)
+    dtype = dtype or (x.dtype if out is None else out.dtype)
+    if dtype not in TYPES:
+        raise SageError("dtype must be float32, bfloat16 or float8_e4m3fn")
+    fp8 = dtype == torch.float8_e4m3fn
+    out = _result(out, (M, -(-d // 16) * 16 if fp8 else d), dtype, x.device)
+    scales = _result(scales, _scale_shape(M, d, "row"), torch.float32, x.device, "scales") if fp8 else None
+    if total is not None or residual is not None:
+        total = _result(total, (M, d), x.dtype, x.device, "total")
+    _check(load_library().sage_rms_norm(_ptr(x), _ptr(residual), TYPES[x.dtype], M, d, _ptr(gain), float(eps),
+                                        _ptr(total), _ptr(out), TYPES[dtype], _ptr(scales), _stream()))
+    return out, scales, total
+
+
+def rms_norm_grad(grad: torch.Tensor, total: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6,
+                  grad_total: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None):
+    """Backward pass of `rms_norm` from the stored sum: (grad_x, grad_gain).
+    grad_x is the gradient of x and of the residual; `grad_total` is what
+    reaches the sum by the residual stream."""
+    _rows(total, "total")
+    _rows(grad, "grad", total)
+    M, d = total.shape
+    _dev(gain, torch.float32, "gain", 1)
+    if gain.shape[0] != d:
+        raise SageError("gain must have one entry per column")
+    if grad_total is not None:
+        _rows(grad_total, "grad_total", total)
+    out = _result(out, (M, d), total.dtype, total.device)
+    grad_gain = torch.empty(d, dtype=torch.float32, device=total.device)
+    lib = load_library()
+    ws = _scratch(workspace, lib.sage_rms_norm_grad_workspace_bytes(M, d), total.device)
+    _check(lib.sage_rms_norm_grad(_ptr(grad), _ptr(total), TYPES[total.dtype], M, d, _ptr(gain), float(eps),
+                                  _ptr(grad_total), _ptr(out), _ptr(grad_gain), _ptr(ws), _size(ws), _stream()))
+    return out, grad_gain
+
+
+def quantize(x: torch.Tensor, block: str = "row", transpose: bool = False, out: Optional[torch.Tensor] = None,
+             scales: Optional[torch.Tensor] = None):
+    """x [M, K], or its transpose, as an 8-bit matrix: (q [R, C rounded up to
+    16] float8_e4m3fn, scales [ceil(C / 128), R or ceil(R / 128)])."""
+    _rows(x, "x")
+    if block not in BLOCKS:
+        raise SageError(f"unknown block {block!r}")
+    M, K = x.shape
+    R, C = (K, M) if transpose else (M, K)
+    out = _result(out, (R, -(-C // 16) * 16), torch.float8_e4m3fn, x.device)
+    scales = _result(scales, _scale_shape(R, C, block), torch.float32, x.device, "scales")
+    _check(load_library().sage_quantize(_ptr(x), TYPES[x.dtype], M, K, BLOCKS[block], int(bool(transpose)), _ptr(out),
+                                        _ptr(scales), _stream()))
+    return out, scales
+
+
+def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
+               bias: Optional[torch.Tensor] = None, relu: bool = False, fast_accum: bool = False,
+               dtype: Optional[torch.dtype] = None, workspace: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out [M, N] = a b^T (+ bias, ReLU) of 8-bit matrices a [M, K] with
+    "row" scales and b [N, K] with "row" or "square" scales (told by their
+    shape), bfloat16 by default. Sums are fp32; `fast_accum` takes the 8-bit
+    matrix instructions, at twice the rate, which add products in groups of 8
+    with about 13 bits below the group's largest."""
+    _dev(a, torch.float8_e4m3fn, "a", 2)
+    _dev(b, torch.float8_e4m3fn, "b", 2)
+    _dev(a_scales, torch.float32, "a_scales", 2)
+    _dev(b_scales, torch.float32, "b_scales", 2)
+    (M, K), N = a.shape, b.shape[0]
+    if b.shape[1] != K:
+        raise SageError("a and b must have rows of one length")
+    if tuple(a_scales.shape) != _scale_shape(M, K, "row"):
+        raise SageError(f"a_scales must be {_scale_shape(M, K, 'row')}, got {tuple(a_scales.shape)}")
+    if tuple(b_scales.shape) not in (_scale_shape(N, K, "row"), _scale_shape(N, K, "square")):
+        raise SageError(f"b_scales must be {_scale_shape(N, K, 'row')} or {_scale_shape(N, K, 'square')}, "
+                        f"got {tuple(b_scales.shape)}")
+    block = "square" if tuple(b_scales.shape) == _scale_shape(N, K, "square") else "row"
+    if bias is not None:
+        _dev(bias, torch.float32, "bias", 1)
+        if bias.shape[0] != N:
+            raise SageError("bias must have one entry per row of b")
+    dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
+    if dtype not in _ROW_TYPES:
+        raise SageError("dtype must be float32 or bfloat16")
+    out = _result(out, (M, N), dtype, a.device)
+    lib = load_library()
+    ws = _scratch(workspace, lib.sage_matmul_fp8_workspace_bytes(M, N, K), a.device)
+    _check(lib.sage_matmul_fp8(_ptr(a), _ptr(a_scales), M, _ptr(b), _ptr(b_scales), BLOCKS[block], N, K, _ptr(bias),
+                               int(bool(relu)), int(bool(fast_accum)), _ptr(out), TYPES[dtype], _ptr(ws), _size(ws), _stream()))
+    return out
 
 
 class Store:

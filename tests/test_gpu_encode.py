@@ -1,0 +1,424 @@
+"""The prompt encoder's operators on the GPU against their definitions in 64
+bits: sizes from one row to many chunks, widths of every residue, prompts and
+rows that are empty, ids that are no tokens, NaN and infinities, shared
+buffers, other streams, graphs."""
+import pytest
+import torch
+
+import tests.encode_ref as ref
+from paper_2603_07917_amd import sage
+from tests.encode_ref import U32, UNIT, close
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, FP8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def tokens_like(T, V, seed, pad=0.0):
+    """Zipf-like: a few ids make up much of the list."""
+    g = gen(seed)
+    ids = (torch.exp(torch.rand(T, generator=g) * float(torch.log(torch.tensor(V + 1.0)))) - 1).int().clamp(0, V - 1)
+    none = torch.rand(T, generator=g) < pad
+    return torch.where(none, torch.where(torch.rand(T, generator=g) < 0.5, torch.tensor(-1), torch.tensor(V)).int(), ids)
+
+
+def cut(T, Q, seed, empty=0.2):
+    """Offsets of Q ragged prompts over all T tokens, some empty."""
+    g = gen(seed)
+    w = torch.exp(1.5 * torch.randn(Q, generator=g)) * (torch.rand(Q, generator=g) >= empty)
+    w[int(torch.randint(0, Q, (1,), generator=g))] += 0.5
+    c = torch.round(torch.cumsum(w.double(), 0) / w.double().sum() * T).int()
+    c[-1] = T
+    return torch.cat([torch.zeros(1, dtype=torch.int32), c])
+
+
+# ------------------------------------------------------------------- lookup
+@pytest.mark.parametrize("T,V,d,ttype,otype", [(1, 1, 1, F32, F32), (3, 7, 5, BF16, F32), (1000, 50, 64, BF16, BF16),
+                                               (77, 500, 1001, BF16, BF16), (2049, 333, 384, F32, BF16),
+                                               (5, 10, 4104, F32, F32), (63, 20, 20000, BF16, BF16)])
+def test_embed_tokens(T, V, d, ttype, otype):
+    tok = tokens_like(T, V, T + d, pad=0.1)
+    table = torch.randn(V, d, generator=gen(d)).to(ttype).cuda()
+    got = sage.embed(tok.cuda(), table, scale=1.7, dtype=otype)
+    want, mag, _ = ref.embed(tok, table, float(torch.tensor(1.7)), None, False)
+    close(got, want, mag * (2 * U32 + UNIT[otype]))
+
+
+@pytest.mark.parametrize("T,Q,V,d,ttype,otype,mean", [
+    (1, 1, 3, 8, BF16, BF16, True), (64, 1, 40, 512, BF16, F32, False), (65, 1, 40, 520, BF16, F32, True),
+    (211, 1, 320, 768, BF16, BF16, True), (5000, 1, 300, 96, F32, F32, False), (3, 9, 5, 40, F32, F32, True),
+    (700, 700, 90, 33, BF16, F32, False), (4096, 64, 1000, 128, BF16, F32, True), (9000, 37, 800, 1001, F32, F32, True),
+    (20000, 3000, 4000, 256, BF16, BF16, False), (70001, 5, 2000, 64, BF16, F32, True), (300, 20, 50, 4100, F32, BF16, False)])
+def test_embed_prompts(T, Q, V, d, ttype, otype, mean):
+    tok, off = tokens_like(T, V, T + Q, pad=0.1), cut(T, Q, T + d)
+    table = torch.randn(V, d, generator=gen(d)).to(ttype).cuda()
+    got = sage.embed(tok.cuda(), table, scale=0.75, offsets=off.cuda(), mean=mean, dtype=otype)
+    want, mag, n = ref.embed(tok, table, 0.75, off, mean)
+    close(got, want, mag * (n + 4) * U32 + want.abs() * UNIT[otype])
+
+
+def test_embed_empty_prompts_and_no_valid_token():
+    table = torch.ones(4, 24, device="cuda")
+    tok = torch.tensor([-1, 9, 2, 3], dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 0, 2, 2, 4, 4], dtype=torch.int32, device="cuda")
+    out = torch.full((5, 24), float("nan"), device="cuda")
+    for mean, top in ((False, 2.0), (True, 1.0)):
+        got = sage.embed(tok, table, offsets=off, mean=mean, out=out).cpu()
+        assert torch.equal(got[:, 0], torch.tensor([0.0, 0.0, 0.0, top, 0.0]))
+        assert torch.equal(got, got[:, :1].expand(5, 24))
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert torch.equal(sage.embed(none, table, offsets=torch.zeros(4, dtype=torch.int32, device="cuda")).cpu(), torch.zeros(3, 24))
+    assert sage.embed(none, table).shape == (0, 24)
+    assert sage.embed(tok, table, offsets=torch.zeros(1, dtype=torch.int32, device="cuda")).shape == (0, 24)
+
+
+def test_embed_prompts_over_a_part_of_the_tokens():
+    tok = tokens_like(900, 60, 3)
+    table = torch.randn(60, 72, generator=gen(4)).cuda()
+    off = torch.tensor([100, 100, 163, 640, 640, 801], dtype=torch.int32)
+    want, mag, n = ref.embed(tok, table, 1.0, off, True)
+    close(sage.embed(tok.cuda(), table, offsets=off.cuda(), mean=True), want, mag * (n + 4) * U32)
+    g = torch.randn(5, 72, generator=gen(5)).cuda()
+    want, mag, n = ref.embed_grad(tok, g, 60, 1.0, off, True, None)
+    close(sage.embed_grad(tok.cuda(), g, 60, offsets=off.cuda(), mean=True), want, mag * (n + 6) * U32)
+
+
+def test_embed_nan_row_stays_in_its_prompt():
+    table = torch.ones(6, 16, device="cuda")
+    table[0] = float("nan")                              # also the row a padding id might read
+    table[4] = float("inf")
+    tok = torch.tensor([1, -1, 2, 0, 3, 4, 5], dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 3, 5, 7], dtype=torch.int32, device="cuda")
+    got = sage.embed(tok, table, offsets=off).cpu()
+    assert torch.equal(got[0], torch.full((16,), 2.0)) and torch.isnan(got[1]).all() and torch.isinf(got[2]).all()
+    assert torch.equal(sage.embed(tok, table)[1].cpu(), torch.zeros(16))
+
+
+# ----------------------------------------------------------- lookup gradient
+GRADS = [(1, 0, 1, 1, F32, False), (5, 0, 3, 40, BF16, False), (1024, 0, 511, 64, BF16, False), (1025, 0, 512, 64, F32, False),
+         (6500, 0, 5003, 77, BF16, False), (30000, 0, 20, 136, F32, False), (4097, 0, 262145, 8, BF16, False),
+         (211, 1, 3200, 768, BF16, True), (3, 9, 5, 40, F32, True), (20000, 300, 3000, 100, F32, True),
+         (50000, 7, 900, 520, BF16, False), (9000, 900, 40, 64, BF16, True)]
+
+
+@pytest.mark.parametrize("T,Q,V,d,gtype,mean", GRADS)
+@pytest.mark.parametrize("held", [None, "apart", "in place"])
+def test_embed_grad(T, Q, V, d, gtype, mean, held):
+    tok = tokens_like(T, V, T + V, pad=0.1)
+    off = cut(T, Q, T) if Q else None
+    g = torch.randn(Q or T, d, generator=gen(d)).to(gtype).cuda()
+    add = torch.randn(V, d, generator=gen(1)).cuda() if held else None
+    want, mag, n = ref.embed_grad(tok, g, V, 1.25, off, mean, add)
+    out = add if held == "in place" else torch.full((V, d), float("nan"), device="cuda")
+    got = sage.embed_grad(tok.cuda(), g, V, scale=1.25, offsets=None if off is None else off.cuda(), mean=mean, add=add, out=out)
+    assert got is out
+    close(got, want, mag * (n + 6) * U32)
+
+
+def test_embed_grad_repeats_bit_for_bit_and_is_the_transpose():
+    T, Q, V, d = 40000, 50, 700, 96
+    tok, off = tokens_like(T, V, 1, pad=0.05).cuda(), cut(T, Q, 2).cuda()
+    g = torch.randn(Q, d, generator=gen(3)).cuda()
+    first = sage.embed_grad(tok, g, V, offsets=off)
+    for _ in range(3):
+        assert torch.equal(sage.embed_grad(tok, g, V, offsets=off), first)
+    # <E, grad> = <embed(E), g> for every E: the lookup is linear, so this is its difference quotient too
+    E = torch.randn(V, d, generator=gen(4)).cuda()
+    out = sage.embed(tok, E, offsets=off)
+    a, b = (E.double() * first.double()).sum(), (out.double() * g.double()).sum()
+    size = (out.double().abs() * g.double().abs()).sum()
+    assert abs(float(a - b)) <= 1e-4 * float(size)
+
+
+def test_embed_grad_of_nothing():
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    add = torch.randn(9, 12, generator=gen(1)).cuda()
+    assert torch.equal(sage.embed_grad(none, torch.empty(0, 12, device="cuda"), 9, add=add), add)
+    assert torch.equal(sage.embed_grad(none, torch.empty(0, 12, device="cuda"), 9).cpu(), torch.zeros(9, 12))
+    tok = torch.full((300,), -1, dtype=torch.int32, device="cuda")
+    assert torch.equal(sage.embed_grad(tok, torch.ones(300, 12, device="cuda"), 9, add=add), add)
+
+
+# --------------------------------------------------------------------- norm
+NORMS = [(1, 1), (3, 5), (8, 768), (2, 100), (300, 128), (77, 130), (50, 256), (65, 384), (33, 512), (20, 1001), (129, 1024),
+         (9, 1600), (7, 2048), (5, 2050), (6, 4096), (4, 5000), (3, 8192), (2, 12345), (2, 16384), (1, 20001), (2, 32768)]
+
+
+def norm_slack(d):
+    """Of n relative to its magnitude: a d-term sum of squares, halved by the root, and 8 roundings."""
+    return (0.5 * d + 8) * U32
+
+
+@pytest.mark.parametrize("M,d", NORMS)
+@pytest.mark.parametrize("xtype,otype", [(BF16, FP8), (F32, FP8), (BF16, BF16), (F32, F32), (BF16, F32)])
+@pytest.mark.parametrize("residual", [True, False])
+def test_rms_norm(M, d, xtype, otype, residual):
+    x = (3 * torch.randn(M, d, generator=gen(d))).to(xtype).cuda()
+    r = torch.randn(M, d, generator=gen(d + 1)).to(xtype).cuda() if residual else None
+    gain = (1 + 0.2 * torch.randn(d, generator=gen(2))).cuda()
+    y, scales, total = sage.rms_norm(x, gain, residual=r, eps=1e-5, dtype=otype)
+    s, n = ref.rms_norm(x, r, gain, float(torch.tensor(1e-5)))
+    if residual:
+        close(total, s, s.abs() * UNIT[xtype], "total")
+    else:
+        assert total is None
+    if otype != FP8:
+        close(y, n, n.abs() * (norm_slack(d) + UNIT[otype]), "out")
+        return
+    kb = -(-d // 128)
+    blocks = torch.nn.functional.pad(n, (0, kb * 128 - d)).view(M, kb, 128)
+    close(scales, (blocks.abs().amax(2) / 448).clamp_min(2.0 ** -126).t(), (blocks.abs().amax(2) / 448).t() * (norm_slack(d) + 2 * U32))
+    assert y.shape == (M, -(-d // 16) * 16) and not y[:, d:].float().cpu().any()
+    step = scales.cpu().double().t().repeat_interleave(128, 1)[:, :d] * 2.0 ** -10
+    close(ref.dequantize(y, scales)[:, :d], n, n.abs() * (2.0 ** -4 + 3 * norm_slack(d)) + step, "out")
+
+
+@pytest.mark.parametrize("otype", [FP8, BF16])
+def test_rms_norm_of_zeros_and_of_what_is_not_finite(otype):
+    x = torch.ones(4, 300, device="cuda")
+    x[0] = 0
+    x[1, 7] = float("nan")
+    x[2, 200] = float("inf")
+    gain = torch.ones(300, device="cuda")
+    y, scales, _ = sage.rms_norm(x, gain, eps=0.0 if otype == BF16 else 1e-6, dtype=otype)
+    v = (ref.dequantize(y, scales) if otype == FP8 else y.cpu().double())
+    if otype == FP8:
+        assert not v[0].any() and not y[:, 300:].float().cpu().any()
+        assert torch.equal(scales[:, 0].cpu(), torch.full((3,), 2.0 ** -126))
+    else:
+        assert torch.isnan(v[0]).all()                   # 0 / 0, as the formula has it without eps
+    assert torch.isnan(v[1, :300]).all()
+    assert torch.isnan(v[2, 200]) and not v[2, :200].any()
+    assert (v[3, :300] - 1).abs().max() < 0.07
+
+
+def test_rms_norm_in_place_of_its_inputs():
+    x, r = torch.randn(70, 384, generator=gen(1)).cuda(), torch.randn(70, 384, generator=gen(2)).cuda()
+    gain = torch.ones(384, device="cuda")
+    y, _, total = sage.rms_norm(x, gain, residual=r)
+    for name in ("x", "residual"):
+        a, b = x.clone(), r.clone()
+        y2, _, t2 = sage.rms_norm(a, gain, residual=b, total=a if name == "x" else b)
+        assert torch.equal(y2, y) and torch.equal(t2, total) and t2 is (a if name == "x" else b)
+
+
+def test_unit_norm_output_for_the_store():
+    x = torch.randn(40, 384, generator=gen(1)).to(BF16).cuda()
+    y, _, _ = sage.rms_norm(x, torch.full((384,), 384 ** -0.5, device="cuda"), eps=0.0, dtype=F32)
+    close(y.double().norm(dim=1), torch.ones(40, dtype=torch.float64), torch.full((40,), 400 * U32))
+
+
+@pytest.mark.parametrize("M,d", NORMS + [(5000, 64), (3001, 520)])
+@pytest.mark.parametrize("xtype", [BF16, F32])
+@pytest.mark.parametrize("stream", [True, False])
+def test_rms_norm_grad(M, d, xtype, stream):
+    s = (2 * torch.randn(M, d, generator=gen(d))).to(xtype).cuda()
+    dy = torch.randn(M, d, generator=gen(d + 1)).to(xtype).cuda()
+    gt = torch.randn(M, d, generator=gen(d + 2)).to(xtype).cuda() if stream else None
+    gain = (1 + 0.2 * torch.randn(d, generator=gen(2))).cuda()
+    dx, dg = sage.rms_norm_grad(dy, s, gain, eps=1e-5, grad_total=gt)
+    dx_, dg_, sx, sg = ref.rms_norm_grad(dy, s, gain, float(torch.tensor(1e-5)), gt)
+    close(dx, dx_, sx * U32 + dx_.abs() * UNIT[xtype], "grad_x")
+    close(dg, dg_, sg * U32, "grad_gain")
+
+
+def test_rms_norm_grad_against_differences():
+    """loss = <c, rms_norm(x, gain)>, along random directions: the quotient's
+    own error is of order h^2 (third derivative) + U32 / h."""
+    M, d, h = 6, 200, 2.0 ** -7
+    x, c = torch.randn(M, d, generator=gen(1)).cuda(), torch.randn(M, d, generator=gen(2)).cuda()
+    gain, v = (1 + 0.2 * torch.randn(d, generator=gen(3))).cuda(), torch.randn(M, d, generator=gen(4)).cuda()
+    vg = torch.randn(d, generator=gen(5)).cuda()
+    loss = lambda a, g: float((sage.rms_norm(a, g)[0].double() * c.double()).sum())
+    dx, dg = sage.rms_norm_grad(c, x, gain)
+    by_x = (loss(x + h * v, gain) - loss(x - h * v, gain)) / (2 * h)
+    by_g = (loss(x, gain + h * vg) - loss(x, gain - h * vg)) / (2 * h)
+    size = float((c.double().abs()).sum())
+    assert abs(by_x - float((dx.double() * v.double()).sum())) <= 4 * (h * h + U32 / h) * size
+    assert abs(by_g - float((dg.double() * vg.double()).sum())) <= 4 * (U32 / h) * size
+
+
+def test_rms_norm_grad_in_place_and_of_nothing():
+    s, dy = torch.randn(50, 264, generator=gen(1)).cuda(), torch.randn(50, 264, generator=gen(2)).cuda()
+    gain = torch.ones(264, device="cuda")
+    dx, dg = sage.rms_norm_grad(dy, s, gain, grad_total=dy)
+    a = dy.clone()
+    dx2, dg2 = sage.rms_norm_grad(a, s, gain, grad_total=a, out=a)
+    assert torch.equal(dx, dx2) and torch.equal(dg, dg2)
+    dx, dg = sage.rms_norm_grad(dy[:0], s[:0], gain)
+    assert dx.shape == (0, 264) and not dg.cpu().any()
+
+
+# ------------------------------------------------------------- 8-bit blocks
+@pytest.mark.parametrize("M,K", [(1, 1), (3, 16), (8, 100), (130, 128), (128, 130), (257, 384), (77, 1001), (1000, 64), (5, 4096)])
+@pytest.mark.parametrize("xtype", [BF16, F32])
+@pytest.mark.parametrize("block", ["row", "square"])
+@pytest.mark.parametrize("transpose", [False, True])
+def test_quantize(M, K, xtype, block, transpose):
+    x = torch.randn(M, K, generator=gen(M + K)) * torch.exp(2 * torch.randn(M, 1, generator=gen(1)))
+    x = x.to(xtype)
+    q, scales = sage.quantize(x.cuda(), block=block, transpose=transpose)
+    want, want_scales = ref.quantize(x, block, transpose)
+    assert torch.equal(scales.cpu(), want_scales)
+    ref.same_e4m3(q, want)
+
+
+def test_quantize_every_e4m3_rounding():
+    """Every fp32 between neighbouring e4m3 values that matters: each midpoint,
+    the values next to it, and the subnormals; the block's top is 448."""
+    v = torch.arange(0, 127, dtype=torch.uint8).view(FP8).float()
+    mid = (v[1:] + v[:-1]) / 2
+    x = torch.cat([v, mid, torch.nextafter(mid, torch.zeros(())), torch.nextafter(mid, torch.full((), 1e9))])
+    x = torch.cat([x, -x])
+    rows = torch.nn.functional.pad(x, (0, -len(x) % 127)).view(-1, 127)
+    rows = torch.cat([torch.full((rows.shape[0], 1), 448.0), rows], 1).contiguous()
+    q, scales = sage.quantize(rows.cuda())
+    assert torch.equal(scales.cpu(), torch.ones_like(scales.cpu()))
+    ref.same_e4m3(q, rows.to(FP8))
+
+
+def test_quantize_what_is_not_finite_and_tiny():
+    x = torch.randn(130, 260, generator=gen(1))
+    x[0, 5], x[1, 130], x[2, 131], x[129, 259] = float("nan"), float("inf"), -float("inf"), float("nan")
+    x[3] = 0
+    x[4] *= 1e-41
+    x[5, :128] = torch.finfo(torch.float32).max
+    for block in ("row", "square"):
+        for transpose in (False, True):
+            q, scales = sage.quantize(x.cuda(), block=block, transpose=transpose)
+            want, want_scales = ref.quantize(x, block, transpose)
+            assert torch.equal(scales.cpu(), want_scales) and torch.isfinite(scales).all()
+            ref.same_e4m3(q, want, (block, transpose))
+
+
+# ------------------------------------------------------------------ product
+PRODUCTS = [(1, 1, 16), (1, 16, 128), (3, 5, 48), (8, 4096, 1024), (16, 130, 272), (17, 257, 4096), (33, 100, 144), (64, 64, 128),
+            (100, 999, 384), (128, 128, 2048), (129, 127, 1008), (250, 300, 16384), (256, 256, 256), (300, 520, 1040),
+            (1000, 1000, 128), (2048, 1536, 640), (3001, 4100, 400)]
+
+
+def operands(M, N, K, block, seed=0):
+    a = torch.randn(M, K, generator=gen(seed + M)) * torch.exp(torch.randn(M, 1, generator=gen(seed + 1)))
+    b = torch.randn(N, K, generator=gen(seed + N + 7)) * torch.exp(0.5 * torch.randn(N, 1, generator=gen(seed + 2)))
+    return *[t.cuda() for t in ref.quantize(a)], *[t.cuda() for t in ref.quantize(b, block)]
+
+
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+@pytest.mark.parametrize("block", ["row", "square"])
+@pytest.mark.parametrize("otype,with_bias,relu", [(BF16, True, True), (F32, False, False), (F32, True, False)])
+def test_matmul(M, N, K, block, otype, with_bias, relu):
+    a, sa, b, sb = operands(M, N, K, block)
+    bias = torch.randn(N, generator=gen(9)).cuda() if with_bias else None
+    got = sage.matmul_fp8(a, sa, b, sb, bias=bias, relu=relu, dtype=otype)
+    want, mag = ref.matmul(a, sa, b, sb, block, bias, relu)
+    # K products and sums, and per block the scales' product, its product with the sum, the addition
+    close(got, want, mag * (K + 4) * U32 + want.abs() * UNIT[otype])
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 16, 128), (33, 100, 144), (100, 999, 384), (129, 127, 1008), (20, 200, 16384),
+                                   (300, 520, 272), (4000, 4096, 16)])
+@pytest.mark.parametrize("block", ["row", "square"])
+@pytest.mark.parametrize("otype", [BF16, F32])
+def test_matmul_fast(M, N, K, block, otype):
+    a, sa, b, sb = operands(M, N, K, block, seed=3)
+    bias = torch.randn(N, generator=gen(9)).cuda()
+    got = sage.matmul_fp8(a, sa, b, sb, bias=bias, fast_accum=True, dtype=otype)
+    want, mag = ref.matmul(a, sa, b, sb, block, bias, False)
+    close(got, want, ref.fast_slack(a, sa, b, sb, block) + mag * (K + 4) * U32 + want.abs() * UNIT[otype])
+
+
+@pytest.mark.parametrize("fast", [False, True])
+def test_matmul_large_tiles_of_small_integers(fast):
+    """Products and sums of small integers are exact in either form: any wrong
+    row, column, block or tail shows. More tiles than the chip has CUs."""
+    M, N, K = 4100, 3500, 400
+    a = torch.randint(-2, 3, (M, K), generator=gen(1)).float()
+    b = torch.randint(-2, 3, (N, K), generator=gen(2)).float()
+    kb = -(-K // 128)
+    sa = 2.0 ** torch.randint(-3, 4, (kb, M), generator=gen(3)).float()
+    sb = 2.0 ** torch.randint(-3, 4, (kb, -(-N // 128)), generator=gen(4)).float()
+    got = sage.matmul_fp8(a.to(FP8).cuda(), sa.cuda(), b.to(FP8).cuda(), sb.cuda(), fast_accum=fast, dtype=F32)
+    want = (a * sa.t().repeat_interleave(128, 1)[:, :K]) @ (b * sb.repeat_interleave(128, 1)[:, :N].t().repeat_interleave(128, 1)[:, :K]).t()
+    assert torch.equal(got.cpu(), want)
+
+
+def test_matmul_one_place_at_a_time():
+    """Single ones, every k of three blocks and a tail, at rows over a whole tile."""
+    K = 416
+    eye = torch.zeros(K, K)
+    eye[torch.arange(K), torch.arange(K)] = 1
+    a, sa = sage.quantize(eye.cuda())
+    b, sb = sage.quantize((1 + torch.arange(300 * K).view(300, K) % 15).float().cuda())
+    got = sage.matmul_fp8(a, sa, b, sb, dtype=F32).cpu().double()
+    # each output is one product: the scales' product and its product with the value, one rounding each
+    want = ref.dequantize(b, sb).t() * (ref.dequantize(a, sa)[0, 0])
+    close(got, want, want.abs() * 4 * U32)
+
+
+def test_matmul_keeps_nan_in_its_row_and_column():
+    a, sa, b, sb = operands(140, 150, 256, "row")
+    a.view(torch.uint8)[7, 200], b.view(torch.uint8)[149, 3] = 0x7F, 0xFF
+    got = sage.matmul_fp8(a, sa, b, sb, relu=True).cpu()
+    nan = torch.zeros(140, 150, dtype=torch.bool)
+    nan[7], nan[:, 149] = True, True
+    assert torch.equal(torch.isnan(got), nan)
+
+
+def test_matmul_gradients_of_a_layer():
+    """grad_x and grad_w of y = x w^T as products of re-laid operands: against
+    the 64-bit products of what the 8-bit operands stand for."""
+    M, N, K = 301, 260, 200
+    x, w, dy = (torch.randn(r, c, generator=gen(r)).cuda() for r, c in ((M, K), (N, K), (M, N)))
+    qd, sd = sage.quantize(dy)
+    wt, swt = sage.quantize(w, block="square", transpose=True)
+    dx = sage.matmul_fp8(qd, sd, wt, swt, dtype=F32)
+    want, mag = ref.matmul(qd, sd, wt, swt, "square", None, False)
+    close(dx, want, mag * (N + 20) * U32)
+    dt, sdt = sage.quantize(dy, transpose=True)
+    xt, sxt = sage.quantize(x, transpose=True)
+    dw = sage.matmul_fp8(dt, sdt, xt, sxt, dtype=F32)
+    want, mag = ref.matmul(dt, sdt, xt, sxt, "row", None, False)
+    close(dw, want, mag * (M + 20) * U32)
+    # and they are the layer's gradients up to the 8-bit rounding of two factors
+    for got, exact in ((dx, dy.double() @ w.double()), (dw, dy.double().t().contiguous() @ x.double())):
+        assert float((got.double() - exact).norm() / exact.norm()) < 2 * 2.0 ** -4
+
+
+# ------------------------------------------------------- streams and graphs
+def test_on_another_stream_and_in_a_graph():
+    T, Q, V, d, N = 3000, 40, 500, 256, 384
+    tok, off = tokens_like(T, V, 1).cuda(), cut(T, Q, 2).cuda()
+    table, w = torch.randn(V, d, generator=gen(3)).to(BF16).cuda(), torch.randn(N, d, generator=gen(4)).cuda()
+    gain = torch.ones(d, device="cuda")
+    wq, ws = sage.quantize(w, block="square")
+
+    def path():
+        e = sage.embed(tok, table, offsets=off, mean=True)
+        q, s, _ = sage.rms_norm(e, gain, dtype=FP8)
+        y = sage.matmul_fp8(q, s, wq, ws, relu=True)
+        dx, dg = sage.rms_norm_grad(e, e, gain)
+        return e, y, dx, dg, sage.embed_grad(tok, e, V, offsets=off, mean=True)
+
+    want = path()
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        got = path()
+    other.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = path()
+    for k in range(3):
+        tok.copy_(tokens_like(T, V, 10 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, path()):
+            assert torch.equal(a, b)
