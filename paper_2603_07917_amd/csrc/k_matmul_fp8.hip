@@ -13,8 +13,7 @@
 // Two forms of P_kb:
 //  * exact products, fp32 sums: e4m3 values become bf16 (exactly) on their way
 //    from LDS to 8 v_mfma_f32_32x32x16_bf16;
-//  * fast: 2 v_mfma_f32_32x32x64_f8f6f4 on the bytes themselves, twice the
-//    rate. That instruction (like the other 8-bit ones) adds its products in
+//  * fast: v_mfma_f32_16x16x128_f8f6f4 on the bytes themselves, twice the rate. That instruction (like the other 8-bit ones) adds its products in
 //    groups of 8 with about 13 bits below the largest of the group (measured:
 //    2^16 + 2^3 is kept, 2^16 + 2^2 is not; between groups sums are fp32), so
 //    a result is off by about 1.4e-5 of its size on normal data: a hundredth
@@ -38,12 +37,37 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 mfma_bf16x8;
 
 __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
 
-// LDS[m0 + size * lane] = `size` bytes at base + off; completion is tracked with wait_loads.
-__device__ __forceinline__ void load16_to_lds(const void* base, uint32_t off, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(off), "s"(base), "s"(m0) : "memory", "m0");
+// Eight pieces of 1 KB (16 bytes a lane) into LDS, from `to` on and `step`
+// apart: four from a + off[0..3], four from b + off[4..7]; then 4 bytes a lane
+// from sc + sc_off to sc_to. Only lanes in `mask` load pieces, and only those
+// in `sc_mask` the last. Completion is tracked with wait_all_loads. One asm
+// block: the loop around it stays one basic block, whose order the compiler
+// keeps. (The waves are full, so all lanes are active before and after.)
+__device__ __forceinline__ void load_pieces(const void* a, const void* b, const uint32_t (&off)[8], uint32_t to,
+                                            uint32_t step, uint64_t mask, const void* sc, uint32_t sc_off,
+                                            uint32_t sc_to, uint64_t sc_mask) {
+  asm volatile(
+      "s_mov_b64 exec, %[mask]\n\ts_mov_b32 m0, %[to]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o0], %[a]\n\t"
+      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o1], %[a]\n\t"
+      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o2], %[a]\n\t"
+      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o3], %[a]\n\t"
+      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o4], %[b]\n\t"
+      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o5], %[b]\n\t"
+      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o6], %[b]\n\t"
+      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o7], %[b]\n\t"
+      "s_mov_b64 exec, %[smask]\n\ts_mov_b32 m0, %[sto]\n\ts_nop 0\n\tglobal_load_lds_dword %[so], %[sc]\n\t"
+      "s_mov_b64 exec, -1"
+      :: [a] "s"(a), [b] "s"(b), [sc] "s"(sc), [to] "s"(to), [sto] "s"(sc_to), [mask] "s"(mask), [smask] "s"(sc_mask),
+         [step] "s"(step), [so] "v"(sc_off), [o0] "v"(off[0]), [o1] "v"(off[1]), [o2] "v"(off[2]), [o3] "v"(off[3]),
+         [o4] "v"(off[4]), [o5] "v"(off[5]), [o6] "v"(off[6]), [o7] "v"(off[7])
+      : "memory", "scc");
 }
-__device__ __forceinline__ void load4_to_lds(const void* base, uint32_t off, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(off), "s"(base), "s"(m0) : "memory", "m0");
+__device__ __forceinline__ uint64_t uniform64(uint32_t lo, uint32_t hi) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)hi) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
+}
+// LDS address of a shared array; the array counts as written by the loads from here on.
+__device__ __forceinline__ uint32_t lds_address(char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)p;
 }
 __device__ __forceinline__ void wait_all_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // Workgroup barrier behind this wave's LDS operations.
@@ -65,118 +89,145 @@ __device__ __forceinline__ Operands to_bf16(intx4 u) {
   }
   return r.o;
 }
-__device__ __forceinline__ floatx16 mfma_e4m3(intx4 a0, intx4 a1, intx4 b0, intx4 b1, floatx16 c) {
-  const intx8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7), b = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7);
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+__device__ __forceinline__ floatx4 mfma_e4m3(const intx8& a, const intx8& b) {
+  const floatx4 zero = {};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);
 }
 
 // Bias, ReLU (a NaN stays one) and the store of 4 neighbouring outputs of a row.
 template <class O, bool kVec>
-__device__ __forceinline__ void finish4(floatx4 y, const float* __restrict__ bias, bool relu, O* row, int n, int N) {
+__device__ __forceinline__ void finish4(floatx4 y, floatx4 bias, bool relu, O* row, int n, int N) {
+  y += bias;
+  if (relu) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (bias && n + j < N) y[j] += bias[n + j];
-    if (relu) y[j] = y[j] < 0.0f ? 0.0f : y[j];
+    for (int j = 0; j < 4; ++j) y[j] = y[j] < 0.0f ? 0.0f : y[j];
   }
   const float v[4] = {y[0], y[1], y[2], y[3]};
   store_row<O, 4, kVec>(v, row, n, N);
 }
+template <bool kVec>
+__device__ __forceinline__ floatx4 bias4(const float* __restrict__ bias, int n, int N) {
+  floatx4 v = {};
+  if (bias) {
+    float f[4];
+    load_row<float, 4, kVec>(f, bias, n, N);
+    v = floatx4{f[0], f[1], f[2], f[3]};
+  }
+  return v;
+}
 
-// One tile of BM rows of a x BN rows of b, over blocks [kb0, kb1) of the summed
-// axis. WM x WN waves.
-template <int BM, int BN, int WM, int WN, bool kFast, bool kSquare, class O, bool kVec>
-__global__ void __launch_bounds__(64 * WM * WN) matmul_fp8_kernel(Fp8Product p, int tiles_m, int tiles_n, int splits,
-                                                                  int blocks_per_split, float* __restrict__ part) {
-  constexpr int kWaves = WM * WN;
-  constexpr int kTileBytes = (BM + BN) * kBlock;
-  constexpr int kStageBytes = kTileBytes + (BM + BN) * 4;
-  constexpr int kPieces = (BM + BN) / 8 / kWaves;        // 8 rows x 128 bytes per load and wave
-  constexpr int MT = BM / WM / 32, NT = BN / WN / 32;    // 32 x 32 tiles of a wave
-  static_assert((BM + BN) / 64 == kWaves && BM % 64 == 0, "64 scales a wave");
+// What a workgroup of W waves computes: BM rows of a x BN rows of b, over blocks
+// [kb0, kb1) of the summed axis; and the loads of its stages in LDS.
+template <int BM, int BN, int W, bool kSquare>
+struct Tile {
+  static constexpr int kTileBytes = (BM + BN) * kBlock;
+  static constexpr int kStageBytes = kTileBytes + (BM + BN) * 4;   // rows of a and of b, then their scales
+  static constexpr int kPieces = (BM + BN) / 8 / W;      // 8 rows x 128 bytes per load and wave
+  static_assert((BM + BN) / 64 == W && BM == BN && kPieces == 8, "four pieces of each operand and 64 scales a wave");
+
+  int m0, n0, kb0, kb1, split;
+  const char *a_base, *b_base;                           // the tile's first rows
+  const float* scale_base;                               // this wave's 64 scales come from here: row kb, entry scale_at
+  uint32_t scale_at;
+  int scale_ld;
+  uint32_t off[kPieces];                                 // this lane's 16 bytes of each piece
+  int full;                                              // whole blocks
+  int tail_chunks;                                       // 16-byte chunks of a row in the block behind them
+  uint64_t tail_lanes;                                   // the lanes whose chunks those are (the same in each piece)
+
+  __device__ __forceinline__ Tile(const Fp8Product& p, int tiles_m, int tiles_n, int splits, int blocks_per_split, int w) {
+    // Workgroup b runs on XCD b % 8. Each XCD takes a run of tiles, and in it
+    // bands of 4 tiles of a, walked along b: the 32 tiles that its CUs work on
+    // at a time are 4 x 8, whose rows its L2 holds.
+    const int total = tiles_m * tiles_n * splits, per = total / 8;
+    int t = blockIdx.x;
+    if (t < per * 8) t = t % 8 * per + t / 8;
+    split = t % splits;
+    t /= splits;
+    const int band = t / (4 * tiles_n), height = min(4, tiles_m - 4 * band);
+    t -= band * 4 * tiles_n;
+    m0 = (4 * band + t % height) * BM;
+    n0 = t / height * BN;
+    const int kblocks = (p.K + kBlock - 1) / kBlock;
+    full = p.K / kBlock;
+    kb0 = split * blocks_per_split;
+    kb1 = min(kblocks, kb0 + blocks_per_split);
+    tail_chunks = p.K % kBlock / 16;
+    a_base = reinterpret_cast<const char*>(p.a) + (long long)m0 * p.K;
+    b_base = reinterpret_cast<const char*>(p.b) + (long long)n0 * p.K;
+    const int lane = (int)lane_id();
+    tail_lanes = __ballot(chunk(0, w, lane) < tail_chunks);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {                  // rows past the end read the last one; their products are not stored
+      const int r = (i * W + w) * 8 + lane / 8;
+      const int row = r < BM ? min(r, p.M - 1 - m0) : min(r - BM, p.N - 1 - n0);
+      off[i] = (uint32_t)row * (uint32_t)p.K + (uint32_t)chunk(i, w, lane) * 16u;
+    }
+    const int r = w * 64 + lane;
+    if (w * 64 < BM) {
+      scale_base = p.a_scales;
+      scale_ld = p.M;
+      scale_at = (uint32_t)min(m0 + r, p.M - 1) * 4u;
+    } else {
+      const int n = min(n0 + r - BM, p.N - 1);
+      scale_base = p.b_scales;
+      scale_ld = kSquare ? (p.N + kBlock - 1) / kBlock : p.N;
+      scale_at = (uint32_t)(kSquare ? n / kBlock : n) * 4u;
+    }
+  }
+  static __device__ __forceinline__ int chunk(int i, int w, int lane) {
+    return (lane % 8) ^ swz((i * W + w) * 8 + lane / 8);
+  }
+  // Block kb into stage st. Of a block that is not whole only the chunks that
+  // the rows have are loaded; of kb >= kb1 nothing.
+  __device__ __forceinline__ void load(uint32_t lds, int kb, int st, int w) const {
+    const uint32_t on = kb < kb1 ? ~0u : 0u;
+    const uint32_t lo = kb < full ? on : on & (uint32_t)tail_lanes, hi = kb < full ? on : on & (uint32_t)(tail_lanes >> 32);
+    load_pieces(a_base + (long long)kb * kBlock, b_base + (long long)kb * kBlock, off, lds + (uint32_t)(st * kStageBytes + w * 8 * kBlock),
+                W * 8 * kBlock, uniform64(lo, hi), scale_base + (long long)kb * scale_ld, scale_at,
+                lds + (uint32_t)(st * kStageBytes + kTileBytes + w * 256), uniform64(on, on));
+  }
+};
+
+// Outputs y of row m, columns n to n + 3.
+template <class O, bool kVec>
+__device__ __forceinline__ void put4(const Fp8Product& p, int splits, int split, float* part, int m, int n, floatx4 y,
+                                     floatx4 bias) {
+  if (m >= p.M || n >= p.N) return;
+  if (splits > 1) finish4<float, kVec>(y, floatx4{}, false, part + ((long long)split * p.M + m) * p.N, n, p.N);
+  else finish4<O, kVec>(y, bias, p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
+}
+
+// The exact form: WM x WN waves of 32 x 32 tiles.
+template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kVec>
+__global__ void __launch_bounds__(64 * WM * WN, 2) matmul_exact_kernel(Fp8Product p, int tiles_m, int tiles_n, int splits,
+                                                                       int blocks_per_split, float* __restrict__ part) {
+  typedef Tile<BM, BN, WM * WN, kSquare> T;
+  constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
   static_assert(BN / WN <= kBlock, "a wave's columns share a square block's scale");
-  __shared__ __attribute__((aligned(16))) char lds[2 * kStageBytes];   // the only one: its byte offsets are LDS addresses
+  __shared__ __attribute__((aligned(16))) char lds[2 * T::kStageBytes];
+  const uint32_t to = lds_address(lds);
   const int lane = (int)lane_id();
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
   const int wm = w % WM, wn = w / WM;
-
-  // Workgroup b runs on XCD b % 8: each XCD takes a run of tiles, n fastest, so
-  // that its L2 holds a few rows of tiles of a and all of b.
-  const int total = tiles_m * tiles_n * splits;
-  int t = blockIdx.x;
-  {
-    const int per = total / 8, x = t % 8;
-    if (t < per * 8) t = x * per + t / 8;
-  }
-  const int split = t % splits;
-  t /= splits;
-  const int m0 = t / tiles_n * BM, n0 = t % tiles_n * BN;
-  const int kblocks = (p.K + kBlock - 1) / kBlock;
-  const int kb0 = split * blocks_per_split, kb1 = min(kblocks, kb0 + blocks_per_split);
-
-  // This lane's source of each piece: row and chunk of a or b (rows past the
-  // end read the last one; their products are not stored).
-  const char* const a_base = reinterpret_cast<const char*>(p.a) + (long long)m0 * p.K;
-  const char* const b_base = reinterpret_cast<const char*>(p.b) + (long long)n0 * p.K;
-  uint32_t off[kPieces];
-  int chunk[kPieces];
-#pragma unroll
-  for (int i = 0; i < kPieces; ++i) {
-    const int r = (i * kWaves + w) * 8 + lane / 8;       // row of the tile, a's first
-    const bool of_a = r < BM;
-    const int row = of_a ? min(r, p.M - 1 - m0) : min(r - BM, p.N - 1 - n0);
-    chunk[i] = (lane % 8) ^ swz(r);
-    off[i] = (uint32_t)row * (uint32_t)p.K + (uint32_t)chunk[i] * 16u;
-  }
-  const int tail_chunks = p.K % kBlock / 16;             // chunks of the last block, 0: all 8
-  auto load_stage = [&](int kb, int st) {
-    const char* const ak = a_base + (long long)kb * kBlock;
-    const char* const bk = b_base + (long long)kb * kBlock;
-    const bool tail = tail_chunks != 0 && kb == kblocks - 1;
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int r0 = (i * kWaves + w) * 8;
-      const uint32_t to = (uint32_t)(st * kStageBytes + r0 * kBlock);
-      if (!tail || chunk[i] < tail_chunks) load16_to_lds(r0 < BM ? ak : bk, off[i], to);
-      else *reinterpret_cast<intx4*>(lds + to + lane * 16) = intx4{};
-    }
-    {                                                    // the block's scales, 64 a wave
-      const int r = w * 64 + lane;
-      const bool of_a = w * 64 < BM;
-      const int n = min(n0 + r - BM, p.N - 1);
-      const float* src = of_a ? p.a_scales + (long long)kb * p.M
-                              : p.b_scales + (long long)kb * (kSquare ? (p.N + kBlock - 1) / kBlock : p.N);
-      const uint32_t at = of_a ? (uint32_t)min(m0 + r, p.M - 1) : (uint32_t)(kSquare ? n / kBlock : n);
-      load4_to_lds(src, at * 4u, (uint32_t)(st * kStageBytes + kTileBytes + w * 256));
-    }
-  };
-
+  const T tile(p, tiles_m, tiles_n, splits, blocks_per_split, w);
   const int l32 = lane & 31, half = lane >> 5;
   floatx16 acc[NT][MT] = {};
-  // Chunk 2 t + half of row r: with the same choice for a and b, the lanes of a
-  // half hold the same k.
-  auto piece = [&](const char* stage, int r, int t) {
-    return *reinterpret_cast<const intx4*>(stage + r * kBlock + (((2 * t + half) ^ swz(r)) * 16));
+  // Chunk 2 t + half of row r0 + l32: the same choice for a and b, so the lanes
+  // of a half hold the same k. Chunks past a row's end are zeros.
+  auto piece = [&](const char* stage, int r0, int t, int chunks) {
+    const intx4 v = *reinterpret_cast<const intx4*>(stage + (r0 + l32) * kBlock + (((2 * t + half) ^ swz(l32)) * 16));
+    return 2 * t + half < chunks ? v : intx4{};
   };
-  if (kb0 < kb1) load_stage(kb0, 0);
-  for (int kb = kb0; kb < kb1; ++kb) {
-    const int st = (kb - kb0) & 1;
-    wait_all_loads();
-    barrier();                                           // this stage has landed; the other one is free
-    if (kb + 1 < kb1) load_stage(kb + 1, st ^ 1);
-    const char* const stage = lds + st * kStageBytes;
-    const float* const sc = reinterpret_cast<const float*>(stage + kTileBytes);
+  auto block = [&](const char* stage, int chunks) {
+    const float* const sc = reinterpret_cast<const float*>(stage + T::kTileBytes);
     float sa[MT];
-    intx4 fa[kFast ? MT : 1][4];
-    Operands wa[kFast ? 1 : MT][4];
+    Operands wa[MT][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int r = (wm * MT + i) * 32 + l32;
-      sa[i] = sc[r];
+      sa[i] = sc[(wm * MT + i) * 32 + l32];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if constexpr (kFast) fa[i][t] = piece(stage, r, t);
-        else wa[i][t] = to_bf16(piece(stage, r, t));
-      }
+      for (int t = 0; t < 4; ++t) wa[i][t] = to_bf16(piece(stage, (wm * MT + i) * 32, t, chunks));
     }
     if constexpr (kSquare) {
       const float sb = sc[BM + wn * NT * 32];
@@ -185,32 +236,24 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fp8_kernel(Fp8Product p, 
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int r = BM + (wn * NT + j) * 32 + l32;
+      const int r0 = BM + (wn * NT + j) * 32;
       intx4 fb[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) fb[t] = piece(stage, r, t);
+      for (int t = 0; t < 4; ++t) fb[t] = piece(stage, r0, t, chunks);
       floatx16 y[MT] = {};
-      if constexpr (kFast) {
 #pragma unroll
-        for (int t = 0; t < 4; t += 2)
+      for (int t = 0; t < 4; ++t) {
+        const Operands wb = to_bf16(fb[t]);
 #pragma unroll
-          for (int i = 0; i < MT; ++i) y[i] = mfma_e4m3(fb[t], fb[t + 1], fa[i][t], fa[i][t + 1], y[i]);
-      } else {
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const Operands wb = to_bf16(fb[t]);
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-              y[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb.v[k], wa[i][t].v[k], y[i], 0, 0, 0);
-        }
+          for (int i = 0; i < MT; ++i)
+            y[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb.v[k], wa[i][t].v[k], y[i], 0, 0, 0);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         floatx4 sb;
-        if constexpr (!kSquare)
-          sb = *reinterpret_cast<const floatx4*>(sc + BM + (wn * NT + j) * 32 + q * 8 + half * 4);
+        if constexpr (!kSquare) sb = *reinterpret_cast<const floatx4*>(sc + r0 + q * 8 + half * 4);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -218,22 +261,166 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fp8_kernel(Fp8Product p, 
             acc[j][i][4 * q + e] = fmaf(y[i][4 * q + e], kSquare ? sa[i] : sa[i] * sb[e], acc[j][i][4 * q + e]);
       }
     }
+  };
+  tile.load(to, tile.kb0, 0, w);
+  const int whole = min(tile.kb1, tile.full);
+  int st = 0;
+  for (int kb = tile.kb0; kb < whole; ++kb, st ^= 1) {
+    wait_all_loads();
+    barrier();                                           // this stage has landed; the other one is free
+    tile.load(to, kb + 1, st ^ 1, w);
+    block(lds + st * T::kStageBytes, 8);
   }
+  if (whole < tile.kb1) {
+    wait_all_loads();
+    barrier();
+    block(lds + st * T::kStageBytes, tile.tail_chunks);
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int n = tile.n0 + (wn * NT + j) * 32 + q * 8 + half * 4;
+      const floatx4 bias = bias4<kVec>(p.bias, n, p.N);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        put4<O, kVec>(p, splits, tile.split, part, tile.m0 + (wm * MT + i) * 32 + l32, n,
+                      floatx4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]}, bias);
+    }
+}
 
+// The fast form: WM x WN waves of 16 x 16 tiles, one MFMA a tile and block.
+// A group is one 16-row tile of b against the wave's MS tiles of a. While a
+// group's MFMAs run, the next group's rows of b are read, and each result is
+// added up kBehind MFMAs later. The block's last two groups run behind the
+// barrier that frees the stage, tile of a by tile of a: a tile's registers take
+// its rows of the next stage as soon as its two MFMAs are issued, so the matrix
+// cores have work while the next block's first rows are read and its
+// successor's loads go out.
+constexpr int kBehind = 2;
+template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kVec>
+__global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p, int tiles_m, int tiles_n, int splits,
+                                                                      int blocks_per_split, float* __restrict__ part) {
+  typedef Tile<BM, BN, WM * WN, kSquare> T;
+  constexpr int MS = BM / WM / 16, NS = BN / WN / 16;
+  static_assert(BN / WN <= kBlock, "a wave's columns share a square block's scale");
+  __shared__ __attribute__((aligned(16))) char lds[2 * T::kStageBytes];
+  const uint32_t to = lds_address(lds);
+  const int lane = (int)lane_id();
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const int wm = w % WM, wn = w / WM;
+  const T tile(p, tiles_m, tiles_n, splits, blocks_per_split, w);
+  const int l16 = lane & 15, g4 = lane >> 4;
+  const int at_a = (wm * MS * 16 + l16) * kBlock, at_b = (BM + wn * NS * 16 + l16) * kBlock;
+  const int lo = (g4 ^ swz(l16)) * 16, hi = ((g4 + 4) ^ swz(l16)) * 16;   // chunks g4 and g4 + 4 of a row
+  auto rows = [&](const char* stage, int at) {
+    const intx4 x = *reinterpret_cast<const intx4*>(stage + at + lo), y = *reinterpret_cast<const intx4*>(stage + at + hi);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  floatx4 acc[NS][MS] = {};
+  intx8 fa[MS], fb[4];                                   // of b: groups j % 4
+  float sa[MS], sa_next[MS];
+  floatx4 sb[4];
+  floatx4 y[kBehind + 1];
+  static_assert(kBehind <= MS && NS % 4 == 0, "a result is added up in the next group at the latest; the rings close with a block");
+  const int at_sa = T::kTileBytes + (wm * MS * 16 + l16) * 4, at_sb = T::kTileBytes + (BM + wn * NS * 16) * 4;
+  auto read_b = [&](const char* stage, int j) {
+    fb[j % 4] = rows(stage, at_b + j * 16 * kBlock);
+    if constexpr (!kSquare) sb[j % 4] = *reinterpret_cast<const floatx4*>(stage + at_sb + j * 64 + g4 * 16);
+  };
+  auto read_scales = [&](const char* stage) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = m0 + (wm * MT + i) * 32 + l32;
-    if (m >= p.M) continue;
+    for (int i = 0; i < MS; ++i) {
+      sa_next[i] = *reinterpret_cast<const float*>(stage + at_sa + i * 64);
+      if constexpr (kSquare) sa_next[i] *= *reinterpret_cast<const float*>(stage + at_sb);
+    }
+  };
+  // MFMA number t of a block; from the last two groups on in the order of a's tiles.
+  constexpr int kMfmas = NS * MS, kLast = (NS - 2) * MS;
+  auto group = [](int t) { return t < kLast ? t / MS : NS - 2 + (t - kLast) % 2; };
+  auto of_a = [](int t) { return t < kLast ? t % MS : (t - kLast) / 2; };
+  auto multiply = [&](int t) { y[t % (kBehind + 1)] = mfma_e4m3(fb[group(t) % 4], fa[of_a(t)]); };
+  auto add_up = [&](int t) {
+    const int j = group(t), i = of_a(t);
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int e = 0; e < 4; ++e)
+      acc[j][i][e] = fmaf(y[t % (kBehind + 1)][e], kSquare ? sa[i] : sa[i] * sb[j % 4][e], acc[j][i][e]);
+    asm volatile("" : "+v"(acc[j][i]));                  // here, and not behind the block with every y alive until then
+  };
+  const int whole = min(tile.kb1, tile.full);
+  int st = 0;
+  tile.load(to, tile.kb0, 0, w);
+  wait_all_loads();
+  barrier();
+  tile.load(to, tile.kb0 + 1, 1, w);
+  read_b(lds, 0);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int n = n0 + (wn * NT + j) * 32 + q * 8 + half * 4;
-        if (n >= p.N) continue;
-        const floatx4 v = {acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
-        if (splits > 1) finish4<float, kVec>(v, nullptr, false, part + ((long long)split * p.M + m) * p.N, n, p.N);
-        else finish4<O, kVec>(v, p.bias, p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
+  for (int i = 0; i < MS; ++i) fa[i] = rows(lds, at_a + i * 16 * kBlock);
+  read_scales(lds);
+  for (int kb = tile.kb0; kb < whole; ++kb, st ^= 1) {
+    const char* const stage = lds + st * T::kStageBytes;
+    const char* const next = lds + (st ^ 1) * T::kStageBytes;
+#pragma unroll
+    for (int i = 0; i < MS; ++i) sa[i] = sa_next[i];
+#pragma unroll
+    for (int j = 0; j < NS - 2; ++j) {
+      read_b(stage, j + 1);
+      if (j == NS - 3) read_b(stage, NS - 1);
+      __builtin_amdgcn_sched_barrier(0);                 // in this order: the compiler's own waits for each result
+#pragma unroll
+      for (int t = j * MS; t < (j + 1) * MS; ++t) {
+        multiply(t);
+        if (t >= kBehind) add_up(t - kBehind);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    wait_all_loads();
+    barrier();                                           // the next stage has landed, this one is free
+    tile.load(to, kb + 2, st, w);
+#pragma unroll
+    for (int t = kLast; t < kMfmas; ++t) {               // past the last block the reads are of a stale stage, never used
+      multiply(t);
+      add_up(t - kBehind);
+      if (t == kLast) read_b(next, 0);
+      if ((t - kLast) % 2) fa[of_a(t)] = rows(next, at_a + of_a(t) * 16 * kBlock);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    read_scales(next);
+#pragma unroll
+    for (int t = kMfmas - kBehind; t < kMfmas; ++t) add_up(t);
+  }
+  if (whole < tile.kb1) {                                // the block that is not whole: chunks past a row's end are zeros
+    const char* const stage = lds + st * T::kStageBytes;
+    auto cut = [&](int at) {
+      intx8 v = rows(stage, at);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = g4 + (k < 4 ? 0 : 4) < tile.tail_chunks ? v[k] : 0;
+      return v;
+    };
+#pragma unroll
+    for (int i = 0; i < MS; ++i) fa[i] = cut(at_a + i * 16 * kBlock);
+    read_scales(stage);
+#pragma unroll
+    for (int i = 0; i < MS; ++i) sa[i] = sa_next[i];
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      read_b(stage, j);
+      const intx8 rows_b = cut(at_b + j * 16 * kBlock);
+#pragma unroll
+      for (int i = 0; i < MS; ++i) {
+        const floatx4 v = mfma_e4m3(rows_b, fa[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][i][e] = fmaf(v[e], kSquare ? sa[i] : sa[i] * sb[j % 4][e], acc[j][i][e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+    const int n = tile.n0 + (wn * NS + j) * 16 + g4 * 4;
+    const floatx4 bias = bias4<kVec>(p.bias, n, p.N);
+#pragma unroll
+    for (int i = 0; i < MS; ++i)
+      put4<O, kVec>(p, splits, tile.split, part, tile.m0 + (wm * MS + i) * 16 + l16, n, acc[j][i], bias);
   }
 }
 
@@ -251,7 +438,7 @@ __global__ void __launch_bounds__(256) matmul_join_kernel(Fp8Product p, int spli
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] += v[j];
   }
-  finish4<O, kVec>(y, p.bias, p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
+  finish4<O, kVec>(y, bias4<kVec>(p.bias, n, p.N), p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
 }
 
 struct Plan {
@@ -275,9 +462,14 @@ template <int BM, int BN, int WM, int WN, bool kFast, bool kSquare, class O, boo
 hipError_t run_tiles(const Fp8Product& p, const Plan& pl, float* part, hipStream_t stream) {
   const int tiles_m = ceil_div(p.M, BM), tiles_n = ceil_div(p.N, BN);
   {
-    LaunchScope scope("matmul_fp8_kernel", stream);
-    matmul_fp8_kernel<BM, BN, WM, WN, kFast, kSquare, O, kVec><<<(unsigned)(tiles_m * tiles_n * pl.splits), 64 * WM * WN, 0, stream>>>(
-        p, tiles_m, tiles_n, pl.splits, pl.blocks_per_split, part);
+    LaunchScope scope(kFast ? "matmul_fast_kernel" : "matmul_exact_kernel", stream);
+    const unsigned grid = (unsigned)(tiles_m * tiles_n * pl.splits);
+    if constexpr (kFast)
+      matmul_fast_kernel<BM, BN, WM, WN, kSquare, O, kVec><<<grid, 64 * WM * WN, 0, stream>>>(
+          p, tiles_m, tiles_n, pl.splits, pl.blocks_per_split, part);
+    else
+      matmul_exact_kernel<BM, BN, WM, WN, kSquare, O, kVec><<<grid, 64 * WM * WN, 0, stream>>>(
+          p, tiles_m, tiles_n, pl.splits, pl.blocks_per_split, part);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1) return e;
   }
