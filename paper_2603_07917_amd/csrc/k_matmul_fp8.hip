@@ -37,30 +37,18 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 mfma_bf16x8;
 
 __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
 
-// Eight pieces of 1 KB (16 bytes a lane) into LDS, from `to` on and `step`
-// apart: four from a + off[0..3], four from b + off[4..7]; then 4 bytes a lane
-// from sc + sc_off to sc_to. Only lanes in `mask` load pieces, and only those
-// in `sc_mask` the last. Completion is tracked with wait_all_loads. One asm
-// block: the loop around it stays one basic block, whose order the compiler
-// keeps. (The waves are full, so all lanes are active before and after.)
-__device__ __forceinline__ void load_pieces(const void* a, const void* b, const uint32_t (&off)[8], uint32_t to,
-                                            uint32_t step, uint64_t mask, const void* sc, uint32_t sc_off,
-                                            uint32_t sc_to, uint64_t sc_mask) {
-  asm volatile(
-      "s_mov_b64 exec, %[mask]\n\ts_mov_b32 m0, %[to]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o0], %[a]\n\t"
-      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o1], %[a]\n\t"
-      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o2], %[a]\n\t"
-      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o3], %[a]\n\t"
-      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o4], %[b]\n\t"
-      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o5], %[b]\n\t"
-      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o6], %[b]\n\t"
-      "s_add_u32 m0, m0, %[step]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[o7], %[b]\n\t"
-      "s_mov_b64 exec, %[smask]\n\ts_mov_b32 m0, %[sto]\n\ts_nop 0\n\tglobal_load_lds_dword %[so], %[sc]\n\t"
-      "s_mov_b64 exec, -1"
-      :: [a] "s"(a), [b] "s"(b), [sc] "s"(sc), [to] "s"(to), [sto] "s"(sc_to), [mask] "s"(mask), [smask] "s"(sc_mask),
-         [step] "s"(step), [so] "v"(sc_off), [o0] "v"(off[0]), [o1] "v"(off[1]), [o2] "v"(off[2]), [o3] "v"(off[3]),
-         [o4] "v"(off[4]), [o5] "v"(off[5]), [o6] "v"(off[6]), [o7] "v"(off[7])
-      : "memory", "scc");
+// LDS[to + 16 * lane] = 16 bytes at base + off, for the lanes in `mask`; the
+// second form 4 bytes. Completion is tracked with wait_all_loads. The lanes are
+// masked inside the asm: the loop around it stays one basic block, whose order
+// the compiler keeps. (The waves are full, so all lanes are active before and
+// after.)
+__device__ __forceinline__ void load16_to_lds(const void* base, uint32_t off, uint32_t to, uint64_t mask) {
+  asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
+               :: "v"(off), "s"(base), "s"(to), "s"(mask) : "memory");
+}
+__device__ __forceinline__ void load4_to_lds(const void* base, uint32_t off, uint32_t to, uint64_t mask) {
+  asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n\ts_mov_b64 exec, -1"
+               :: "v"(off), "s"(base), "s"(to), "s"(mask) : "memory");
 }
 __device__ __forceinline__ uint64_t uniform64(uint32_t lo, uint32_t hi) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)hi) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
@@ -178,14 +166,22 @@ struct Tile {
   static __device__ __forceinline__ int chunk(int i, int w, int lane) {
     return (lane % 8) ^ swz((i * W + w) * 8 + lane / 8);
   }
-  // Block kb into stage st. Of a block that is not whole only the chunks that
-  // the rows have are loaded; of kb >= kb1 nothing.
-  __device__ __forceinline__ void load(uint32_t lds, int kb, int st, int w) const {
+  // Piece i (8: the scales) of block kb into stage st. Of a block that is not
+  // whole only the chunks that the rows have are loaded; of kb >= kb1 nothing.
+  __device__ __forceinline__ void load(uint32_t lds, int kb, int st, int w, int i) const {
     const uint32_t on = kb < kb1 ? ~0u : 0u;
-    const uint32_t lo = kb < full ? on : on & (uint32_t)tail_lanes, hi = kb < full ? on : on & (uint32_t)(tail_lanes >> 32);
-    load_pieces(a_base + (long long)kb * kBlock, b_base + (long long)kb * kBlock, off, lds + (uint32_t)(st * kStageBytes + w * 8 * kBlock),
-                W * 8 * kBlock, uniform64(lo, hi), scale_base + (long long)kb * scale_ld, scale_at,
-                lds + (uint32_t)(st * kStageBytes + kTileBytes + w * 256), uniform64(on, on));
+    if (i < kPieces) {
+      const uint32_t lo = kb < full ? on : on & (uint32_t)tail_lanes, hi = kb < full ? on : on & (uint32_t)(tail_lanes >> 32);
+      load16_to_lds((i < kPieces / 2 ? a_base : b_base) + (long long)kb * kBlock, off[i],
+                    lds + (uint32_t)(st * kStageBytes + (i * W + w) * 8 * kBlock), uniform64(lo, hi));
+    } else {
+      load4_to_lds(scale_base + (long long)kb * scale_ld, scale_at, lds + (uint32_t)(st * kStageBytes + kTileBytes + w * 256),
+                   uniform64(on, on));
+    }
+  }
+  __device__ __forceinline__ void load_all(uint32_t lds, int kb, int st, int w) const {
+#pragma unroll
+    for (int i = 0; i <= kPieces; ++i) load(lds, kb, st, w, i);
   }
 };
 
@@ -262,13 +258,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) matmul_exact_kernel(Fp8Produc
       }
     }
   };
-  tile.load(to, tile.kb0, 0, w);
+  tile.load_all(to, tile.kb0, 0, w);
   const int whole = min(tile.kb1, tile.full);
   int st = 0;
   for (int kb = tile.kb0; kb < whole; ++kb, st ^= 1) {
     wait_all_loads();
     barrier();                                           // this stage has landed; the other one is free
-    tile.load(to, kb + 1, st ^ 1, w);
+    tile.load_all(to, kb + 1, st ^ 1, w);
     block(lds + st * T::kStageBytes, 8);
   }
   if (whole < tile.kb1) {
@@ -291,18 +287,24 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) matmul_exact_kernel(Fp8Produc
 
 // The fast form: WM x WN waves of 16 x 16 tiles, one MFMA a tile and block.
 // A group is one 16-row tile of b against the wave's MS tiles of a. While a
-// group's MFMAs run, the next group's rows of b are read, and each result is
-// added up kBehind MFMAs later. The block's last two groups run behind the
+// group's MFMAs run, the rows of b of the group after the next are read, and each
+// result is added up kBehind MFMAs later. The block's last two groups run behind the
 // barrier that frees the stage, tile of a by tile of a: a tile's registers take
 // its rows of the next stage as soon as its two MFMAs are issued, so the matrix
-// cores have work while the next block's first rows are read and its
-// successor's loads go out.
-constexpr int kBehind = 2;
+// cores have work while the next block's first rows are read. The loads of the
+// block after that go out one by one, the first MS behind the barrier and the
+// others in the next block: as a burst of 9 they fill the address unit's queue,
+// and the waves wait there with their MFMAs behind.
+constexpr int kBehind = 3;
 template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kVec>
 __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p, int tiles_m, int tiles_n, int splits,
                                                                       int blocks_per_split, float* __restrict__ part) {
   typedef Tile<BM, BN, WM * WN, kSquare> T;
   constexpr int MS = BM / WM / 16, NS = BN / WN / 16;
+  constexpr int kMfmas = NS * MS, kLast = (NS - 2) * MS;   // MFMAs of a block, and those before the barrier
+  constexpr int kEarly = MS;                             // pieces of the next stage that are loaded behind the barrier
+  constexpr int kLate = T::kPieces + 1 - kEarly, kGap = 2 * kLate <= kLast ? 2 : 1;   // the others, every kGap MFMAs
+  static_assert(kGap * kLate <= kLast, "before the next barrier");
   static_assert(BN / WN <= kBlock, "a wave's columns share a square block's scale");
   __shared__ __attribute__((aligned(16))) char lds[2 * T::kStageBytes];
   const uint32_t to = lds_address(lds);
@@ -335,25 +337,32 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
       if constexpr (kSquare) sa_next[i] *= *reinterpret_cast<const float*>(stage + at_sb);
     }
   };
-  // MFMA number t of a block; from the last two groups on in the order of a's tiles.
-  constexpr int kMfmas = NS * MS, kLast = (NS - 2) * MS;
+  // MFMA number t of a block is of this group and tile of a: the last two groups in the order of a's tiles.
   auto group = [](int t) { return t < kLast ? t / MS : NS - 2 + (t - kLast) % 2; };
   auto of_a = [](int t) { return t < kLast ? t % MS : (t - kLast) / 2; };
-  auto multiply = [&](int t) { y[t % (kBehind + 1)] = mfma_e4m3(fb[group(t) % 4], fa[of_a(t)]); };
+  // The empty asm statements keep the MFMAs and the additions where they stand;
+  // left to the compiler, an MFMA moves down to its addition, or the additions
+  // behind the block with every y alive until then.
+  auto multiply = [&](int t) {
+    y[t % (kBehind + 1)] = mfma_e4m3(fb[group(t) % 4], fa[of_a(t)]);
+    asm volatile("" : "+v"(y[t % (kBehind + 1)]));
+  };
   auto add_up = [&](int t) {
     const int j = group(t), i = of_a(t);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       acc[j][i][e] = fmaf(y[t % (kBehind + 1)][e], kSquare ? sa[i] : sa[i] * sb[j % 4][e], acc[j][i][e]);
-    asm volatile("" : "+v"(acc[j][i]));                  // here, and not behind the block with every y alive until then
+    asm volatile("" : "+v"(acc[j][i]));
   };
   const int whole = min(tile.kb1, tile.full);
   int st = 0;
-  tile.load(to, tile.kb0, 0, w);
+  tile.load_all(to, tile.kb0, 0, w);
   wait_all_loads();
   barrier();
-  tile.load(to, tile.kb0 + 1, 1, w);
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i) tile.load(to, tile.kb0 + 1, 1, w, i);
   read_b(lds, 0);
+  read_b(lds, 1);
 #pragma unroll
   for (int i = 0; i < MS; ++i) fa[i] = rows(lds, at_a + i * 16 * kBlock);
   read_scales(lds);
@@ -364,24 +373,25 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
     for (int i = 0; i < MS; ++i) sa[i] = sa_next[i];
 #pragma unroll
     for (int j = 0; j < NS - 2; ++j) {
-      read_b(stage, j + 1);
-      if (j == NS - 3) read_b(stage, NS - 1);
+      read_b(stage, j + 2);
       __builtin_amdgcn_sched_barrier(0);                 // in this order: the compiler's own waits for each result
 #pragma unroll
       for (int t = j * MS; t < (j + 1) * MS; ++t) {
         multiply(t);
         if (t >= kBehind) add_up(t - kBehind);
+        if (t % kGap == kGap - 1 && t / kGap < kLate) tile.load(to, kb + 1, st ^ 1, w, kEarly + t / kGap);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     wait_all_loads();
     barrier();                                           // the next stage has landed, this one is free
-    tile.load(to, kb + 2, st, w);
 #pragma unroll
     for (int t = kLast; t < kMfmas; ++t) {               // past the last block the reads are of a stale stage, never used
       multiply(t);
       add_up(t - kBehind);
       if (t == kLast) read_b(next, 0);
+      if (t == kLast + kBehind) read_b(next, 1);         // its scales' registers: group NS - 3's last result is added
+      if (t % 2 == 0) tile.load(to, kb + 2, st, w, (t - kLast) / 2);
       if ((t - kLast) % 2) fa[of_a(t)] = rows(next, at_a + of_a(t) * 16 * kBlock);
       __builtin_amdgcn_sched_barrier(0);
     }
