@@ -8,18 +8,25 @@
 // consecutive segments (prompts; equal tokens of the sorted list), and a sum
 // per segment. The list is cut into chunks of equal length whatever the
 // segments, so that one long prompt, or the few tokens that make up most of a
-// text, are spread over the chip. A wave walks a chunk, keeps the running sum
-// of 16 bytes of columns per lane in fp32, and writes a segment's sum when it
-// ends; a segment that crosses chunks leaves one partial sum per chunk, which
-// a second kernel adds in order. No atomics on values: results do not depend
-// on the order in which waves run.
+// text, are spread over the chip. 16 lanes walk a chunk, keep the running sum
+// of 256 bytes of columns in fp32, and write a segment's sum when it ends; a
+// segment that crosses chunks leaves one partial sum per chunk, which a second
+// kernel adds in order. No atomics on values: results do not depend on the
+// order in which waves run.
+//
+// Bound by the gather. Text repeats its tokens (and a gradient its prompts), so
+// each XCD takes its own columns: the 256-byte pieces of eight times as many
+// rows stay in its L2.
+#include <type_traits>
+
 #include "sage_encode.hpp"
 #include "sage_internal.hpp"
 
 namespace sage {
 namespace {
 
-constexpr int kTurn = 8;                                 // rows in flight per wave
+constexpr int kGroup = 16;                               // lanes per row piece
+constexpr int kTurn = 8;                                 // rows in flight per lane group
 
 // ------------------------------------------------------- lookup per token
 // Each thread copies pieces of 8 columns; a workgroup owns kRows tokens.
@@ -40,22 +47,38 @@ __global__ void __launch_bounds__(256) embed_tokens_kernel(const int32_t* __rest
   }
 }
 
+// Prompt of each token (-1: none), for the kernels below, which ask several
+// times; and the rows of prompts without tokens. A workgroup takes 2,048 tokens
+// and searches between their first and last prompts.
+constexpr int kPromptTokens = 2048;
+__device__ __forceinline__ int last_at_most(const int32_t* __restrict__ offsets, int lo, int hi, int i) {
+  while (hi - lo > 1) {                                  // offsets[lo] <= i < offsets[hi]
+    const int mid = (lo + hi) >> 1;
+    if (offsets[mid] <= i) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+__global__ void __launch_bounds__(256) prompt_of_kernel(const int32_t* __restrict__ offsets, int T, int Q,
+                                                        int32_t* __restrict__ prompt) {
+  const int first = blockIdx.x * kPromptTokens, last = min(first + kPromptTokens, T) - 1;
+  const int begin = offsets[0], end = offsets[Q];
+  int lo = 0, hi = Q;
+  if (begin <= last && first < end) {
+    lo = last_at_most(offsets, 0, Q, max(first, begin));
+    hi = last_at_most(offsets, 0, Q, min(last, end - 1)) + 1;
+  }
+  for (int i = first + (int)threadIdx.x; i <= last; i += 256)
+    prompt[i] = i >= begin && i < end ? last_at_most(offsets, lo, hi, i) : -1;
+}
+
 // ------------------------------------------------------------ list of items
 // Item i of the list: its segment (-1: none), its source row (-1: adds
 // nothing, but its segment exists) and its weight.
 struct PromptItems {                                     // tokens in order, by prompt
-  const int32_t *tokens, *offsets;
-  int T, Q, V;
-  __device__ __forceinline__ int bag(int i) const {      // last q with offsets[q] <= i
-    int lo = 0, hi = Q;                                  // offsets[lo] <= i < offsets[hi], as offsets[0] = 0, offsets[Q] = T
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (offsets[mid] <= i) lo = mid; else hi = mid;
-    }
-    return lo;
-  }
-  __device__ __forceinline__ bool any(int i) const { return i >= 0 && i < T && i >= offsets[0] && i < offsets[Q]; }
-  __device__ __forceinline__ int segment(int i) const { return any(i) ? bag(i) : -1; }
+  static constexpr bool kWeighted = false;
+  const int32_t *tokens, *prompt;                        // prompt of each token, or -1
+  int T, V;
+  __device__ __forceinline__ int segment(int i) const { return i >= 0 && i < T ? prompt[i] : -1; }
   __device__ __forceinline__ int source(int i) const {
     const int id = tokens[i];
     return (unsigned)id < (unsigned)V ? id : -1;
@@ -63,6 +86,7 @@ struct PromptItems {                                     // tokens in order, by 
   __device__ __forceinline__ float weight(int) const { return 1.0f; }
 };
 struct SortedItems {                                     // token positions or prompts, by token
+  static constexpr bool kWeighted = true;
   const uint32_t *keys, *rows;
   const int32_t* valid;                                  // valid tokens per prompt (mean), or null
   int T, V;
@@ -75,30 +99,59 @@ struct SortedItems {                                     // token positions or p
   __device__ __forceinline__ float weight(int i) const { return valid ? __fdiv_rn(1.0f, (float)valid[rows[i]]) : 1.0f; }
 };
 
-// The columns of a lane: V consecutive ones, or (unaligned rows) every 64th,
-// so that neighbouring lanes read neighbouring elements.
+// The columns of a lane in piece p of a row: V = 16 bytes of consecutive ones,
+// or (unaligned rows) every 16th, so that neighbouring lanes read neighbouring
+// elements. Kept as loaded; to_f32 gives the values.
 template <class T, int V, bool kAligned>
-__device__ __forceinline__ void load_cols(float (&v)[V], const T* row, int slice, int d) {
-  const int lane = (int)lane_id();
+struct Cols {
+  union {
+    uint4 bits;
+    T t[V];
+  };
+  __device__ __forceinline__ void load(const T* row, int piece, int d) {
+    const int l = (int)lane_id() % kGroup;
+    if constexpr (kAligned) {
+      const int c = (piece * kGroup + l) * V;
+      bits = c < d ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int c = (piece * V + j) * kGroup + l;
+        t[j] = c < d ? row[c] : (T)0.0f;
+      }
+    }
+  }
+  __device__ __forceinline__ void add_to(float (&acc)[V]) const {
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] += (float)t[j];
+  }
+  __device__ __forceinline__ void add_to(float (&acc)[V], float w) const {
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] = fmaf((float)t[j], w, acc[j]);
+  }
+};
+template <int V, bool kAligned>
+__device__ __forceinline__ void load_cols(float (&v)[V], const float* row, int piece, int d) {
+  const int l = (int)lane_id() % kGroup;
   if constexpr (kAligned) {
-    load_row<T, V, true>(v, row, slice * 64 * V + lane * V, d);
+    load_row<float, V, true>(v, row, (piece * kGroup + l) * V, d);
   } else {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int c = (slice * V + j) * 64 + lane;
-      v[j] = c < d ? (float)row[c] : 0.0f;
+      const int c = (piece * V + j) * kGroup + l;
+      v[j] = c < d ? row[c] : 0.0f;
     }
   }
 }
 template <class T, int V, bool kAligned>
-__device__ __forceinline__ void store_cols(const float (&v)[V], T* row, int slice, int d) {
-  const int lane = (int)lane_id();
+__device__ __forceinline__ void store_cols(const float (&v)[V], T* row, int piece, int d) {
+  const int l = (int)lane_id() % kGroup;
   if constexpr (kAligned) {
-    store_row<T, V, true>(v, row, slice * 64 * V + lane * V, d);
+    store_row<T, V, true>(v, row, (piece * kGroup + l) * V, d);
   } else {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const int c = (slice * V + j) * 64 + lane;
+      const int c = (piece * V + j) * kGroup + l;
       if (c < d) row[c] = (T)v[j];
     }
   }
@@ -106,14 +159,24 @@ __device__ __forceinline__ void store_cols(const float (&v)[V], T* row, int slic
 
 // Partial sums: two rows of d fp32 per chunk, [0] of the segment that was open
 // when the chunk began, [1] of the one that began in it and goes on after it;
-// and their counts of valid items. tail[c] is the segment of [1], or -1.
+// and their counts of valid items. head[c] and tail[c] are their segments, or -1.
 struct Partials {
   float* sum;
-  int32_t* count;
-  int32_t* tail;
+  int32_t *count, *head, *tail;
 };
+// A gradient's table passes by once, and should not push the rows that the sums
+// gather out of the L2s (131,072 x 1,024 with add: 407 -> 389 us).
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+__device__ __forceinline__ floatx4 stream_load(const float* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(p));
+}
+__device__ __forceinline__ void stream_store(floatx4 v, float* p) {
+  __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(p));
+}
+
 // What a finished sum becomes: (x scale, / count for a mean) + add, rounded.
-template <class O>
+// kStream: the rows pass by once.
+template <class O, bool kStream>
 struct Finish {
   O* out;
   const float* add;                                      // fp32 rows like out, or null
@@ -121,148 +184,340 @@ struct Finish {
   bool mean;
   int d;
   template <int V, bool kAligned>
-  __device__ __forceinline__ void write(const float (&acc)[V], int count, int seg, int slice) const {
+  __device__ __forceinline__ void load_add(float (&held)[V], int seg, int piece) const {
+    const float* row = add + (long long)seg * d;
+    if constexpr (kStream && kAligned) {
+      const int c = (piece * kGroup + (int)lane_id() % kGroup) * V;
+      if (c >= d) return;
+#pragma unroll
+      for (int j = 0; j < V; j += 4) {
+        const floatx4 q = stream_load(row + c + j);
+        held[j] = q[0], held[j + 1] = q[1], held[j + 2] = q[2], held[j + 3] = q[3];
+      }
+    } else {
+      load_cols<V, kAligned>(held, row, piece, d);
+    }
+  }
+  template <int V, bool kAligned>
+  __device__ __forceinline__ void write(const float (&acc)[V], const float (&held)[V], int count, int seg, int piece) const {
     const float c = mean && count > 0 ? __fdiv_rn(scale, (float)count) : scale;
     float v[V];
-    if (add) {
-      load_cols<float, V, kAligned>(v, add + (long long)seg * d, slice, d);
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = fmaf(acc[j], c, v[j]);
+    for (int j = 0; j < V; ++j) v[j] = add ? fmaf(acc[j], c, held[j]) : acc[j] * c;
+    O* row = out + (long long)seg * d;
+    if constexpr (kStream && kAligned) {
+      const int at = (piece * kGroup + (int)lane_id() % kGroup) * V;
+      if (at >= d) return;
+#pragma unroll
+      for (int j = 0; j < V; j += 4) stream_store(floatx4{v[j], v[j + 1], v[j + 2], v[j + 3]}, row + at + j);
     } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = acc[j] * c;
+      store_cols<O, V, kAligned>(v, row, piece, d);
     }
-    store_cols<O, V, kAligned>(v, out + (long long)seg * d, slice, d);
   }
 };
 
-// One wave per (chunk of `chunk` items, slice of 64 V columns); `chunk` is a
-// multiple of 64, and lane l holds item l of the 64 in work.
-template <class Items, class T, class O, int V, bool kAligned>
-__global__ void __launch_bounds__(256) segment_sum_kernel(Items items, const T* __restrict__ src, int d, int slices,
-                                                          int chunk, int chunks, Partials part, Finish<O> fin) {
-  const int lane = (int)lane_id();
-  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64));
-  const int c = wave / slices, slice = wave % slices;
-  if (c >= chunks) return;                               // whole waves, no barrier below
-  const int begin = c * chunk;
-  int cur = items.segment(begin - 1);                    // the open segment, if the chunk's first items are its
-  bool open = true;                                      // whether the running segment began before the chunk
-  {
-    const int s0 = items.segment(begin);
-    if (s0 != cur || s0 < 0) open = false;
-    cur = s0;
+// The work of a launch: (piece, chunk) pairs, 16 chunks of one piece per
+// workgroup, piece by piece in runs per XCD (workgroup b runs on XCD b % 8).
+struct ChunkGrid {
+  int chunk, chunks, pieces;
+  __host__ __device__ int rows() const { return (chunks + 15) / 16; }      // workgroups per piece
+  __host__ __device__ long long groups() const { return ((long long)rows() * pieces + 7) / 8 * 8; }
+  // (piece, first chunk) of workgroup b, or piece -1.
+  __device__ __forceinline__ int2 at(unsigned b, long long groups) const {
+    const long long t = (long long)(b % 8) * (groups / 8) + b / 8;
+    if (t >= (long long)rows() * pieces) return make_int2(-1, 0);
+    return make_int2((int)(t / rows()), (int)(t % rows()) * 16);
   }
+};
+
+// The value of lane kLane of each 16, in all of them.
+template <int kLane>
+__device__ __forceinline__ int of_lane(int x) {
+  return __builtin_amdgcn_mov_dpp(x, 0x150 + kLane, 0xf, 0xf, true);
+}
+template <int kLane, class F>
+__device__ __forceinline__ void each_lane(F&& f) {       // f(integral_constant) for 0 .. kLane - 1
+  if constexpr (kLane > 0) {
+    each_lane<kLane - 1>(f);
+    f(std::integral_constant<int, kLane - 1>{});
+  }
+}
+
+// The sums of the chunks c0 .. c0 + 15 of one piece: 16 lanes each, `chunk` a
+// multiple of 16; lane l of a group holds item l of the 16 in work. With kAdd
+// the rows of `add` that finished segments need are loaded beside the items':
+// most tokens of a text are rare, and a load of its own for each would wait.
+template <bool kAdd, class Items, class T, class F, int V, bool kAligned>
+__device__ __forceinline__ void sum_chunks(const Items& items, const T* __restrict__ src, int d, const ChunkGrid& grid,
+                                           int piece, int c0, const Partials& part, const F& fin) {
+  constexpr int kTurn = kAdd && V > 4 ? 4 : 8;           // rows in flight per group
+  const int l = (int)lane_id() % kGroup;
+  const int c = c0 + (int)threadIdx.x / kGroup;
+  const bool mine = c < grid.chunks;                     // the wave's other groups may have a chunk: stay
+  const int begin = mine ? c * grid.chunk : items.T;     // segment(T) is none
+  int cur = items.segment(begin);
+  bool open = cur >= 0 && items.segment(begin - 1) == cur;   // whether the running segment began before the chunk
+  if (mine && piece == 0 && l == 0) part.head[c] = open ? cur : -1;
   float acc[V] = {};
   int count = 0;
-  auto flush = [&](bool goes_on) {
-    if (cur >= 0) {
-      if (open || goes_on) {
-        const long long slot = 2LL * c + (open ? 0 : 1);
-        store_cols<float, V, kAligned>(acc, part.sum + slot * d, slice, d);
-        if (lane == 0 && slice == 0) part.count[slot] = count;
-      } else {
-        fin.template write<V, kAligned>(acc, count, cur, slice);
-      }
+  auto flush = [&](bool goes_on, const float (&held)[V]) {
+    if (cur < 0) return;
+    if (open || goes_on) {
+      const long long slot = 2LL * c + (open ? 0 : 1);
+      store_cols<float, V, kAligned>(acc, part.sum + slot * d, piece, d);
+      if (piece == 0 && l == 0) part.count[slot] = count;
+    } else {
+      fin.template write<V, kAligned>(acc, held, count, cur, piece);
     }
   };
-  for (int base = begin; base < begin + chunk; base += 64) {
-    const int i = base + lane;
-    const int seg = items.segment(i);
+  float held[V] = {};                                    // add's row of the running segment, where its last item is behind
+  int seg_next = mine ? items.segment(begin + l) : -1;
+  for (int base = 0; base < grid.chunk; base += kGroup) {
+    const int i = mine ? begin + base + l : items.T;
+    const int seg = seg_next;
+    seg_next = mine ? items.segment(i + kGroup) : -1;
     const int row = seg >= 0 ? items.source(i) : -1;
-    const float wgt = row >= 0 ? items.weight(i) : 0.0f;
-    if (__all(seg < 0) && cur < 0) continue;
-    for (int j0 = 0; j0 < 64; j0 += kTurn) {
-      float v[kTurn][V];
-#pragma unroll
-      for (int u = 0; u < kTurn; ++u) {
-        const int r = __builtin_amdgcn_readlane(row, j0 + u);
-        load_cols<T, V, kAligned>(v[u], src + (long long)max(r, 0) * d, slice, d);
-      }
-#pragma unroll
-      for (int u = 0; u < kTurn; ++u) {
-        const int s = __builtin_amdgcn_readlane(seg, j0 + u);
-        if (s != cur) {
-          flush(false);
-          cur = s;
-          open = false;
-          count = 0;
-#pragma unroll
-          for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+    const float wgt = Items::kWeighted && row >= 0 ? items.weight(i) : 1.0f;
+    // Whether the item is the last of its segment: the next one's segment, lane by lane.
+    const int after = __shfl_down(seg, 1, kGroup), after_all = __shfl(seg_next, 0, kGroup);
+    const bool last = seg >= 0 && (l == kGroup - 1 ? after_all : after) != seg;
+    const int add_of = kAdd && last ? seg : -1;
+    const bool all_valid = __all(row >= 0);
+    if (!all_valid && !__any(row >= 0) && !__any(seg != cur)) continue;   // e.g. behind the list's end
+    // The usual 16 items of prompts: valid, and of the segments that the groups are in.
+    const bool steady = all_valid && __all(seg == cur);
+    auto turn = [&](auto at) {
+      constexpr int j0 = decltype(at)::value;
+      Cols<T, V, kAligned> v[kTurn];
+      float more[kAdd ? kTurn : 1][V];
+      each_lane<kTurn>([&](auto u) {
+        constexpr int k = decltype(u)::value, j = j0 + k;
+        v[k].load(src + (long long)max(of_lane<j>(row), 0) * d, piece, d);
+        if constexpr (kAdd) {
+          const int s = of_lane<j>(add_of);
+          if (s >= 0) fin.template load_add<V, kAligned>(more[k], s, piece);
         }
-        if (__builtin_amdgcn_readlane(row, j0 + u) >= 0) {
-          const float x = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(wgt), j0 + u));
-          ++count;
+      });
+      each_lane<kTurn>([&](auto u) {
+        constexpr int k = decltype(u)::value, j = j0 + k;
+        if (!steady) {
+          const int s = of_lane<j>(seg);
+          if (s != cur) {
+            flush(false, held);
+            cur = s;
+            open = false;
+            count = 0;
 #pragma unroll
-          for (int j = 0; j < V; ++j) acc[j] = fmaf(v[u][j], x, acc[j]);
+            for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+          }
+        }
+        if constexpr (kAdd) {
+          if (of_lane<j>(add_of) >= 0) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) held[e] = more[k][e];
+          }
+        }
+        if (!steady && of_lane<j>(row) < 0) return;
+        ++count;
+        if constexpr (Items::kWeighted) v[k].add_to(acc, __int_as_float(of_lane<j>(__float_as_int(wgt))));
+        else v[k].add_to(acc);
+      });
+    };
+    each_lane<kGroup / kTurn>([&](auto t) { turn(std::integral_constant<int, decltype(t)::value * kTurn>{}); });
+  }
+  if (!mine) return;
+  const bool goes_on = cur >= 0 && items.segment(begin + grid.chunk) == cur;
+  if (piece == 0 && l == 0) part.tail[c] = goes_on && !open ? cur : -1;
+  flush(goes_on, held);
+}
+
+// The segments that cross chunks: 16 lanes for each (chunk where one begins,
+// piece) add its partial sums in order. One of more than 16 further chunks is
+// left to the whole workgroup, whose 16 groups take every 16th chunk, four at a
+// time.
+template <class F, int V, bool kAligned>
+__global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid, Partials part, F fin) {
+  __shared__ float sums[16][kGroup * V];
+  __shared__ int counts[16];
+  __shared__ int long_run[16];
+  const int l = threadIdx.x % kGroup, g = threadIdx.x / kGroup;
+  const int piece = blockIdx.x / grid.rows(), c0 = blockIdx.x % grid.rows() * 16;
+  {
+    const int c = c0 + g;
+    const int seg = c < grid.chunks ? part.tail[c] : -1;
+    const int mine = seg >= 0 && c + 1 + l < grid.chunks && part.head[c + 1 + l] == seg;
+    const uint64_t runs = __ballot(mine);
+    const uint32_t run = (uint32_t)(runs >> (g % 4 * kGroup)) & 0xFFFFu;   // lane i: chunk c + 1 + i is its
+    if (l == 0) long_run[g] = run == 0xFFFFu;
+    if (seg >= 0 && run != 0xFFFFu) {
+      const int n = __builtin_ctz(~run);                 // 1 to 15 further chunks
+      float acc[V];
+      load_cols<V, kAligned>(acc, part.sum + (2LL * c + 1) * d, piece, d);
+      int count = part.count[2LL * c + 1];
+      float held[V] = {};
+      if (fin.add) fin.template load_add<V, kAligned>(held, seg, piece);
+      for (int k0 = 0; k0 < n; k0 += 4) {
+        float v[4][V];
+        int m[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int k = c + 1 + min(k0 + u, n - 1);
+          load_cols<V, kAligned>(v[u], part.sum + 2LL * k * d, piece, d);
+          m[u] = part.count[2LL * k];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (k0 + u >= n) continue;
+          count += m[u];
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[j] += v[u][j];
         }
       }
+      fin.template write<V, kAligned>(acc, held, count, seg, piece);
     }
   }
-  const bool goes_on = cur >= 0 && items.segment(begin + chunk) == cur;
-  if (slice == 0 && lane == 0) part.tail[c] = goes_on && !open ? cur : -1;
-  flush(goes_on);
-}
-
-// The segments that cross chunks: the wave of the chunk where one begins adds
-// its partial sums, chunk by chunk. part.tail of a later chunk tells nothing
-// about where a segment ends: the items do.
-template <class Items, class T, class O, int V, bool kAligned>
-__global__ void __launch_bounds__(256) segment_join_kernel(Items items, int d, int slices, int chunk, int chunks,
-                                                           Partials part, Finish<O> fin) {
-  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64));
-  const int c = wave / slices, slice = wave % slices;
-  if (c >= chunks) return;
-  const int seg = part.tail[c];
-  if (seg < 0) return;
-  float acc[V];
-  load_cols<float, V, kAligned>(acc, part.sum + (2LL * c + 1) * d, slice, d);
-  int count = part.count[2LL * c + 1];
-  for (int k = c + 1; k < chunks && items.segment(k * chunk) == seg; ++k) {
-    float v[V];
-    load_cols<float, V, kAligned>(v, part.sum + 2LL * k * d, slice, d);
-    count += part.count[2LL * k];
+  __syncthreads();
+  for (int s = 0; s < 16; ++s) {
+    if (!long_run[s]) continue;                          // the same for all threads
+    const int c = c0 + s, seg = part.tail[c];
+    float acc[V] = {};
+    int count = 0;
+    if (g == 0) {
+      load_cols<V, kAligned>(acc, part.sum + (2LL * c + 1) * d, piece, d);
+      count = part.count[2LL * c + 1];
+    }
+    bool more = true;
+    for (int k0 = c + 1; more && k0 < grid.chunks; k0 += 64) {
+      float v[4][V] = {};
+      int n[4] = {};
+      bool in = false;
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += v[j];
+      for (int u = 0; u < 4; ++u) {
+        const int k = k0 + u * 16 + g;
+        in = k < grid.chunks && part.head[k] == seg;
+        if (in) {
+          load_cols<V, kAligned>(v[u], part.sum + 2LL * k * d, piece, d);
+          n[u] = part.count[2LL * k];
+        }
+      }
+      more = __syncthreads_and(in);                      // whether all of the last 16 are still the segment's
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        count += n[u];
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += v[u][j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sums[g][l * V + j] = acc[j];
+    if (l == 0) counts[g] = count;
+    __syncthreads();
+    if (g == 0) {
+      for (int i = 1; i < 16; ++i) {
+        count += counts[i];
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += sums[i][l * V + j];
+      }
+      float held[V] = {};
+      if (fin.add) fin.template load_add<V, kAligned>(held, seg, piece);
+      fin.template write<V, kAligned>(acc, held, count, seg, piece);
+    }
+    __syncthreads();
   }
-  fin.template write<V, kAligned>(acc, count, seg, slice);
 }
 
-// Prompts with no tokens: rows of zeros.
-template <class O, int V, bool kAligned>
-__global__ void __launch_bounds__(256) empty_prompts_kernel(const int32_t* __restrict__ offsets, int T, int Q, int d,
-                                                            int slices, Finish<O> fin) {
-  const int q = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64));
-  if (q >= Q) return;
-  const int b = max(offsets[q], 0), e = min(offsets[q + 1], T);
-  if (b < e) return;
+// Prompts: the chunks' sums, and (workgroups behind them) zeros for the prompts
+// that have no tokens, 16 a workgroup.
+template <class T, class O, int V, bool kAligned>
+__global__ void __launch_bounds__(256) prompt_sum_kernel(PromptItems items, const int32_t* __restrict__ offsets, int Q,
+                                                         const T* __restrict__ src, int d, ChunkGrid grid,
+                                                         unsigned sum_groups, Partials part, Finish<O, false> fin) {
+  if (blockIdx.x < sum_groups) {
+    const int2 at = grid.at(blockIdx.x, sum_groups);
+    if (at.x >= 0) sum_chunks<false, PromptItems, T, Finish<O, false>, V, kAligned>(items, src, d, grid, at.x, at.y, part, fin);
+    return;
+  }
+  const int q = (int)(blockIdx.x - sum_groups) * 16 + (int)threadIdx.x / kGroup;
+  if (q >= Q || max(offsets[q], 0) < min(offsets[q + 1], items.T)) return;
   const float zero[V] = {};
-  for (int s = 0; s < slices; ++s) fin.template write<V, kAligned>(zero, 0, q, s);
+  for (int p = 0; p < grid.pieces; ++p) fin.template write<V, kAligned>(zero, zero, 0, q, p);
 }
 
-// Tokens that the list does not have: rows of zeros, or of `add`. A wave takes
-// 32 rows: lane l finds the first item of token v0 + l by a binary search.
-template <int V, bool kAligned>
-__global__ void __launch_bounds__(256) missing_tokens_kernel(const uint32_t* __restrict__ keys, int T, int n_rows,
-                                                             int d, int slices, Finish<float> fin) {
+// Few tokens: a workgroup per prompt and piece, whose 16 lane groups take every
+// 16th token. One launch, no partial sums in memory.
+template <class T, class O, int V, bool kAligned>
+__global__ void __launch_bounds__(256) prompt_whole_kernel(PromptItems items, const int32_t* __restrict__ offsets,
+                                                           const T* __restrict__ src, int d, int pieces, Finish<O, false> fin) {
+  __shared__ float sums[16][kGroup * V];
+  __shared__ int counts[16];
+  const int q = blockIdx.x / pieces, piece = blockIdx.x % pieces;
+  const int l = threadIdx.x % kGroup, g = threadIdx.x / kGroup;
+  const int b = max(offsets[q], 0), e = min(offsets[q + 1], items.T);
+  float acc[V] = {};
+  int count = 0;
+  for (int i0 = b + g; i0 < e; i0 += 16 * kTurn) {
+    Cols<T, V, kAligned> v[kTurn];
+    int row[kTurn];
+#pragma unroll
+    for (int u = 0; u < kTurn; ++u) row[u] = i0 + u * 16 < e ? items.source(i0 + u * 16) : -1;
+#pragma unroll
+    for (int u = 0; u < kTurn; ++u)
+      if (row[u] >= 0) v[u].load(src + (long long)row[u] * d, piece, d);
+#pragma unroll
+    for (int u = 0; u < kTurn; ++u)
+      if (row[u] >= 0) {
+        v[u].add_to(acc);
+        ++count;
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) sums[g][l * V + j] = acc[j];
+  if (l == 0) counts[g] = count;
+  __syncthreads();
+  if (g > 0) return;
+  for (int i = 1; i < 16; ++i) {
+    count += counts[i];
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] += sums[i][l * V + j];
+  }
+  const float held[V] = {};
+  fin.template write<V, kAligned>(acc, held, count, q, piece);
+}
+
+// Tokens: the chunks' sums, and (workgroups behind them) the rows of tokens
+// that the list does not have, zeros or `add`: 128 rows a workgroup, 32 a wave,
+// whose lane i finds the first item of its token i by a binary search.
+template <bool kAdd, class T, int V, bool kAligned>
+__global__ void __launch_bounds__(256) token_sum_kernel(SortedItems items, const T* __restrict__ src, int d, ChunkGrid grid,
+                                                        unsigned sum_groups, Partials part, Finish<float, true> fin) {
+  if (blockIdx.x < sum_groups) {
+    const int2 at = grid.at(blockIdx.x, sum_groups);
+    if (at.x >= 0) sum_chunks<kAdd, SortedItems, T, Finish<float, true>, V, kAligned>(items, src, d, grid, at.x, at.y, part, fin);
+    return;
+  }
   constexpr int kTake = 32;
   const int lane = (int)lane_id();
-  const int wave = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + threadIdx.x / 64));
-  const int v0 = wave * kTake;
-  if (v0 >= n_rows) return;
-  int lo = 0, hi = T;
-  const uint32_t want = (uint32_t)min(v0 + min(lane, kTake), n_rows);
+  const long long first = ((long long)(blockIdx.x - sum_groups) * 4 + threadIdx.x / 64) * kTake;
+  if (first >= items.V) return;
+  const int v0 = (int)first;
+  int lo = 0, hi = items.T;
+  const uint32_t want = (uint32_t)min(v0 + min(lane, kTake), items.V);
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
-    if (keys[mid] >= want) hi = mid; else lo = mid + 1;
+    if (items.keys[mid] >= want) hi = mid; else lo = mid + 1;
   }
   const int next = __shfl_down(lo, 1, 64);
-  uint64_t missing = __ballot(lane < kTake && v0 + lane < n_rows && lo == next);
-  const float zero[V] = {};
+  uint64_t missing = __ballot(lane < kTake && v0 + lane < items.V && lo == next);
   while (missing) {
-    const int l = __builtin_ctzll(missing);
+    const int v = v0 + __builtin_ctzll(missing);
     missing &= missing - 1;
-    for (int s = 0; s < slices; ++s) fin.template write<V, kAligned>(zero, 0, v0 + l, s);
+    const long long at = (long long)v * d;
+    if (kAligned) {
+      for (int c = lane * 4; c < d; c += 256)
+        stream_store(fin.add ? stream_load(fin.add + at + c) : floatx4{}, fin.out + at + c);
+    } else {
+      for (int c = lane; c < d; c += 64) fin.out[at + c] = fin.add ? fin.add[at + c] : 0.0f;
+    }
   }
 }
 
@@ -281,7 +536,7 @@ constexpr int kSortTile = kSortThreads * kSortItems;
 // Key of token i: V for one outside the table or (with prompts) in none of them.
 __device__ __forceinline__ uint32_t token_key(const PromptItems& p, int i) {
   const int id = p.tokens[i];
-  return (unsigned)id < (unsigned)p.V && (!p.offsets || p.any(i)) ? (uint32_t)id : (uint32_t)p.V;
+  return (unsigned)id < (unsigned)p.V && (!p.prompt || p.prompt[i] >= 0) ? (uint32_t)id : (uint32_t)p.V;
 }
 
 // kFirst: the keys come from the tokens, and (mean) each prompt's valid tokens
@@ -302,7 +557,7 @@ __global__ void __launch_bounds__(kSortThreads) token_count_kernel(PromptItems p
       atomicAdd(&cnt[(k >> shift) & (kSortBins - 1)], 1u);
     }
     if (kFirst && valid) {
-      const int q = i < T && k < (uint32_t)prompts.V ? prompts.segment(i) : -1;
+      const int q = i < T && k < (uint32_t)prompts.V ? prompts.prompt[i] : -1;
       uint64_t left = __ballot(q >= 0);
       while (left) {
         const int q0 = __builtin_amdgcn_readlane(q, __builtin_ctzll(left));
@@ -360,7 +615,7 @@ __global__ void __launch_bounds__(kSortThreads) token_scatter_kernel(
     key[it] = i >= T ? 0u : kFirst ? token_key(prompts, i) : keys[i];
     if (i >= T) val[it] = 0u;
     else if (!kFirst) val[it] = rows[i];
-    else val[it] = prompts.offsets ? (uint32_t)max(prompts.segment(i), 0) : (uint32_t)i;
+    else val[it] = prompts.prompt ? (uint32_t)max(prompts.prompt[i], 0) : (uint32_t)i;
   }
   // Exclusive scan of the digit totals, two per thread, plus this tile's offset.
   {
@@ -428,55 +683,57 @@ __global__ void __launch_bounds__(256) clear_kernel(int32_t* __restrict__ p, int
 }
 
 // ------------------------------------------------------------------- plans
-// Items per chunk: about eight waves per SIMD over all chunks and slices, in
-// whole groups of 64.
-int chunk_items(int T, int slices) {
-  const long long want = (long long)T * slices / 8192;
-  return (int)min(1024LL, max(64LL, (want + 63) / 64 * 64));
+// Items per chunk: about 8,192 waves (eight per SIMD) over all chunks and
+// pieces, in whole groups of 16.
+int chunk_items(int T, int pieces) {
+  const long long want = (long long)T * pieces / 32768;
+  return (int)min(1024LL, max(16LL, (want + 15) / 16 * 16));
 }
-// Slices of 64 lanes x 16 bytes of source columns.
-int slice_count(int d, int vec) { return ceil_div(d, 64 * vec); }
+int piece_count(int d, int vec) { return ceil_div(d, kGroup * vec); }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 struct PartialLayout {
-  int chunk, chunks;
-  size_t sum, count, tail, bytes;
+  ChunkGrid grid;
+  size_t sum, count, head, tail, bytes;
 };
-// For the narrower slices of fp32 sources, which have the smaller chunks' bound.
 PartialLayout partial_layout(int T, int d, int vec) {
   PartialLayout l{};
-  l.chunk = chunk_items(T, slice_count(d, vec));
-  l.chunks = ceil_div(T, l.chunk);
+  l.grid.pieces = piece_count(d, vec);
+  l.grid.chunk = chunk_items(T, l.grid.pieces);
+  l.grid.chunks = ceil_div(T, l.grid.chunk);
   l.sum = 0;
-  l.count = align256(2ull * l.chunks * d * sizeof(float));
-  l.tail = l.count + align256(2ull * l.chunks * sizeof(int32_t));
-  l.bytes = l.tail + align256((size_t)l.chunks * sizeof(int32_t));
+  l.count = align256(2ull * l.grid.chunks * d * sizeof(float));
+  l.head = l.count + align256(2ull * l.grid.chunks * sizeof(int32_t));
+  l.tail = l.head + align256((size_t)l.grid.chunks * sizeof(int32_t));
+  l.bytes = l.tail + align256((size_t)l.grid.chunks * sizeof(int32_t));
   return l;
 }
+// Of either source type.
 size_t partial_bytes(int T, int d) { return max(partial_layout(T, d, 4).bytes, partial_layout(T, d, 8).bytes); }
 Partials partials_at(void* ws, const PartialLayout& l) {
   char* p = static_cast<char*>(ws);
   return Partials{reinterpret_cast<float*>(p + l.sum), reinterpret_cast<int32_t*>(p + l.count),
-                  reinterpret_cast<int32_t*>(p + l.tail)};
+                  reinterpret_cast<int32_t*>(p + l.head), reinterpret_cast<int32_t*>(p + l.tail)};
 }
 
-template <class Items, class T, class O, int V, bool kAligned>
-hipError_t sum_segments(const Items& items, int n, const T* src, int d, void* ws, const Finish<O>& fin,
-                        hipStream_t stream) {
-  const int slices = slice_count(d, V);
-  const PartialLayout l = partial_layout(n, d, V);
-  const Partials part = partials_at(ws, l);
-  const unsigned grid = (unsigned)(((long long)l.chunks * slices + 3) / 4);
-  {
-    LaunchScope scope("segment_sum_kernel", stream);
-    segment_sum_kernel<Items, T, O, V, kAligned><<<grid, 256, 0, stream>>>(items, src, d, slices, l.chunk, l.chunks, part, fin);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
+template <class F, int V, bool kAligned>
+hipError_t join_segments(int d, const PartialLayout& l, const Partials& part, const F& fin,
+                         hipStream_t stream) {
+  if (l.grid.chunks <= 1) return hipSuccess;
   LaunchScope scope("segment_join_kernel", stream);
-  segment_join_kernel<Items, T, O, V, kAligned><<<grid, 256, 0, stream>>>(items, d, slices, l.chunk, l.chunks, part, fin);
+  segment_join_kernel<F, V, kAligned><<<(unsigned)l.grid.rows() * l.grid.pieces, 256, 0, stream>>>(d, l.grid, part, fin);
   return hipGetLastError();
 }
+
+hipError_t find_prompts(const int32_t* offsets, int T, int Q, int32_t* prompt, hipStream_t stream) {
+  LaunchScope scope("prompt_of_kernel", stream);
+  prompt_of_kernel<<<ceil_div(T, kPromptTokens), 256, 0, stream>>>(offsets, T, Q, prompt);
+  return hipGetLastError();
+}
+
+// Few tokens of few prompts: a workgroup per prompt adds them (a prompt that has
+// them all is 32 turns of it).
+constexpr int kWholeTokens = 4096, kWholeGroups = 4096;
 
 template <class T, class O, bool kAligned>
 hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, int d, float scale, Prompts p, void* out,
@@ -490,16 +747,30 @@ hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, i
     embed_tokens_kernel<T, O, kAligned><<<ceil_div(T_, rows), 256, 0, stream>>>(tokens, T_, src, V, d, rows, scale, dst);
     return hipGetLastError();
   }
-  const Finish<O> fin{dst, nullptr, scale, p.mean, d};
-  const int slices = slice_count(d, kVec);
-  {
-    LaunchScope scope("empty_prompts_kernel", stream);
-    empty_prompts_kernel<O, kVec, kAligned><<<ceil_div(p.Q, 4), 256, 0, stream>>>(p.offsets, T_, p.Q, d, slices, fin);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || T_ == 0) return e;
+  const Finish<O, false> fin{dst, nullptr, scale, p.mean, d};
+  const int pieces = piece_count(d, kVec);
+  if (T_ <= kWholeTokens && (long long)p.Q * pieces <= kWholeGroups) {
+    LaunchScope scope("prompt_whole_kernel", stream);
+    prompt_whole_kernel<T, O, kVec, kAligned><<<(unsigned)p.Q * pieces, 256, 0, stream>>>(
+        PromptItems{tokens, nullptr, T_, V}, p.offsets, src, d, pieces, fin);
+    return hipGetLastError();
   }
-  const PromptItems items{tokens, p.offsets, T_, p.Q, V};
-  return sum_segments<PromptItems, T, O, kVec, kAligned>(items, T_, src, d, ws, fin, stream);
+  const PartialLayout l = partial_layout(T_, d, kVec);
+  const Partials part = partials_at(ws, l);
+  int32_t* prompt = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + partial_bytes(T_, d));
+  const PromptItems items{tokens, prompt, T_, V};
+  if (T_ > 0) {
+    const hipError_t e = find_prompts(p.offsets, T_, p.Q, prompt, stream);
+    if (e != hipSuccess) return e;
+  }
+  {
+    LaunchScope scope("prompt_sum_kernel", stream);
+    const unsigned groups = (unsigned)l.grid.groups();
+    prompt_sum_kernel<T, O, kVec, kAligned><<<groups + ceil_div(p.Q, 16), 256, 0, stream>>>(items, p.offsets, p.Q, src, d, l.grid, groups, part, fin);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return join_segments<Finish<O, false>, kVec, kAligned>(d, l, part, fin, stream);
 }
 
 template <class T, class O>
@@ -516,7 +787,7 @@ int key_bits(int V) {                                    // keys are 0..V
 }
 struct GradLayout {
   int tiles;
-  size_t keys[2], rows[2], hist, total, valid, part, bytes;
+  size_t keys[2], rows[2], hist, total, prompt, valid, part, bytes;
 };
 GradLayout grad_layout(int T, int Q, int d) {
   GradLayout l{};
@@ -532,6 +803,8 @@ GradLayout grad_layout(int T, int Q, int d) {
   at += align256((size_t)kSortBins * l.tiles * 4);
   l.total = at;
   at += align256(kSortBins * 4);
+  l.prompt = at;
+  at += Q > 0 ? align256((size_t)T * 4) : 0;
   l.valid = at;
   at += align256((size_t)Q * 4);
   l.part = at;
@@ -550,10 +823,11 @@ hipError_t embed_grad_with(const int32_t* tokens, int T_, const void* grad, int 
   uint32_t* hist = reinterpret_cast<uint32_t*>(base + l.hist);
   uint32_t* total = reinterpret_cast<uint32_t*>(base + l.total);
   int32_t* valid = p.offsets && p.mean ? reinterpret_cast<int32_t*>(base + l.valid) : nullptr;
-  const Finish<float> fin{out, add, scale, false, d};
-  const int slices = slice_count(d, kVec);
-  const PromptItems prompts{tokens, p.offsets, T_, p.Q, V};
+  const Finish<float, true> fin{out, add, scale, false, d};
+  int32_t* prompt = p.offsets ? reinterpret_cast<int32_t*>(base + l.prompt) : nullptr;
+  const PromptItems prompts{tokens, prompt, T_, V};
   hipError_t e;
+  if (prompt && T_ > 0 && (e = find_prompts(p.offsets, T_, p.Q, prompt, stream)) != hipSuccess) return e;
   if (valid && T_ > 0) {
     LaunchScope scope("clear_kernel", stream);
     clear_kernel<<<ceil_div(p.Q, 256), 256, 0, stream>>>(valid, p.Q);
@@ -586,19 +860,25 @@ hipError_t embed_grad_with(const int32_t* tokens, int T_, const void* grad, int 
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (add != out) {                                      // in place, rows with no token stay as they are
-    LaunchScope scope("missing_tokens_kernel", stream);
-    missing_tokens_kernel<kVec, kAligned><<<ceil_div(ceil_div(V, 32), 4), 256, 0, stream>>>(keys[at], T_, V, d, slices, fin);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  const SortedItems items{keys[at], rows[at], valid, T_, V};
+  const PartialLayout pl = partial_layout(T_, d, kVec);
+  const Partials part = partials_at(base + l.part, pl);
+  const unsigned groups = T_ > 0 ? (unsigned)pl.grid.groups() : 0;
+  const unsigned fill = add != out ? (unsigned)ceil_div(V, 128) : 0;   // in place, rows with no token stay as they are
+  if (groups + fill > 0) {
+    LaunchScope scope("token_sum_kernel", stream);
+    const T* src = static_cast<const T*>(grad);
+    if (add) token_sum_kernel<true, T, kVec, kAligned><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
+    else token_sum_kernel<false, T, kVec, kAligned><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
+    if ((e = hipGetLastError()) != hipSuccess || T_ == 0) return e;
   }
   if (T_ == 0) return hipSuccess;
-  const SortedItems items{keys[at], rows[at], valid, T_, V};
-  return sum_segments<SortedItems, T, float, kVec, kAligned>(items, T_, static_cast<const T*>(grad), d, base + l.part, fin, stream);
+  return join_segments<Finish<float, true>, kVec, kAligned>(d, pl, part, fin, stream);
 }
 
 }  // namespace
 
-size_t embed_workspace_bytes(int T, int Q, int d) { return T > 0 && Q > 0 ? partial_bytes(T, d) : 0; }
+size_t embed_workspace_bytes(int T, int Q, int d) { return T > 0 && Q > 0 ? partial_bytes(T, d) + align256((size_t)T * 4) : 0; }
 
 hipError_t launch_embed(const int32_t* tokens, int T, const void* table, Type table_type, int V, int d, float scale,
                         Prompts p, void* out, Type out_type, void* ws, hipStream_t stream) {

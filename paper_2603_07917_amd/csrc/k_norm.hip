@@ -231,8 +231,10 @@ __global__ void __launch_bounds__(1024) norm_gain_kernel(const float* __restrict
   __shared__ float sums[16][64];
   const int c = threadIdx.x % 64, g = threadIdx.x / 64, col = blockIdx.x * 64 + c;
   float t = 0.0f;
-  if (col < d)
+  if (col < d) {
+#pragma unroll 8
     for (int r = g; r < rows; r += 16) t += part[(long long)r * d + col];
+  }
   sums[g][c] = t;
   __syncthreads();
   if (g == 0 && col < d) {
