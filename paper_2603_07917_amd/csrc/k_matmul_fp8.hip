@@ -46,18 +46,15 @@ __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
 // after.)
 __device__ __forceinline__ void load16_to_lds(const void* base, uint32_t off, uint32_t to, uint64_t mask) {
   asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
-               :: "v"(off), "s"(base), "s"(to), "s"(mask) : "memory");
+               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane((int)to)), "s"(mask) : "memory");
 }
 __device__ __forceinline__ void load4_to_lds(const void* base, uint32_t off, uint32_t to, uint64_t mask) {
   asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n\ts_mov_b64 exec, -1"
-               :: "v"(off), "s"(base), "s"(to), "s"(mask) : "memory");
-}
-__device__ __forceinline__ uint64_t uniform64(uint32_t lo, uint32_t hi) {
-  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)hi) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
+               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane((int)to)), "s"(mask) : "memory");
 }
 // LDS address of a shared array; the array counts as written by the loads from here on.
 __device__ __forceinline__ uint32_t lds_address(char* p) {
-  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)p;
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)p);
 }
 __device__ __forceinline__ void wait_all_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // Workgroup barrier behind this wave's LDS operations.
@@ -110,205 +107,12 @@ __device__ __forceinline__ floatx4 bias4(const float* __restrict__ bias, int n, 
   return v;
 }
 
-// What a workgroup of W waves computes: BM rows of a x BN rows of b, over blocks
-// [kb0, kb1) of the summed axis; and the loads of its stages in LDS.
-template <int BM, int BN, int W, bool kSquare>
-struct Tile {
-  static constexpr int kTileBytes = (BM + BN) * kBlock;
-  static constexpr int kStageBytes = kTileBytes + (BM + BN) * 4;   // rows of a and of b, then their scales
-  static constexpr int kPieces = (BM + BN) / 8 / W;      // 8 rows x 128 bytes per load and wave
-  static_assert((BM + BN) / 64 == W && BM == BN && kPieces == 8, "four pieces of each operand and 64 scales a wave");
-
-  int m0, n0, kb0, kb1, split;
-  const char *a_base, *b_base;                           // the tile's first rows
-  const float* scale_base;                               // this wave's 64 scales come from here: row kb, entry scale_at
-  uint32_t scale_at;
-  int scale_ld;
-  uint32_t off[kPieces];                                 // this lane's 16 bytes of each piece
-  int full;                                              // whole blocks
-  int tail_chunks;                                       // 16-byte chunks of a row in the block behind them
-  uint64_t tail_lanes;                                   // the lanes whose chunks those are (the same in each piece)
-
-  __device__ __forceinline__ Tile(const Fp8Product& p, int tiles_m, int tiles_n, int splits, int blocks_per_split, int w) {
-    // Workgroup b runs on XCD b % 8. Each XCD takes a run of tiles, and in it
-    // bands of 4 tiles of a, walked along b: the 32 tiles that its CUs work on
-    // at a time are 4 x 8, whose rows its L2 holds.
-    const int total = tiles_m * tiles_n * splits, per = total / 8;
-    int t = blockIdx.x;
-    if (t < per * 8) t = t % 8 * per + t / 8;
-    split = t % splits;
-    t /= splits;
-    const int band = t / (4 * tiles_n), height = min(4, tiles_m - 4 * band);
-    t -= band * 4 * tiles_n;
-    m0 = (4 * band + t % height) * BM;
-    n0 = t / height * BN;
-    const int kblocks = (p.K + kBlock - 1) / kBlock;
-    full = p.K / kBlock;
-    kb0 = split * blocks_per_split;
-    kb1 = min(kblocks, kb0 + blocks_per_split);
-    tail_chunks = p.K % kBlock / 16;
-    a_base = reinterpret_cast<const char*>(p.a) + (long long)m0 * p.K;
-    b_base = reinterpret_cast<const char*>(p.b) + (long long)n0 * p.K;
-    const int lane = (int)lane_id();
-    tail_lanes = __ballot(chunk(0, w, lane) < tail_chunks);
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {                  // rows past the end read the last one; their products are not stored
-      const int r = (i * W + w) * 8 + lane / 8;
-      const int row = r < BM ? min(r, p.M - 1 - m0) : min(r - BM, p.N - 1 - n0);
-      off[i] = (uint32_t)row * (uint32_t)p.K + (uint32_t)chunk(i, w, lane) * 16u;
-    }
-    const int r = w * 64 + lane;
-    if (w * 64 < BM) {
-      scale_base = p.a_scales;
-      scale_ld = p.M;
-      scale_at = (uint32_t)min(m0 + r, p.M - 1) * 4u;
-    } else {
-      const int n = min(n0 + r - BM, p.N - 1);
-      scale_base = p.b_scales;
-      scale_ld = kSquare ? (p.N + kBlock - 1) / kBlock : p.N;
-      scale_at = (uint32_t)(kSquare ? n / kBlock : n) * 4u;
-    }
-  }
-  static __device__ __forceinline__ int chunk(int i, int w, int lane) {
-    return (lane % 8) ^ swz((i * W + w) * 8 + lane / 8);
-  }
-  // Piece i (8: the scales) of block kb into stage st. Of a block that is not
-  // whole only the chunks that the rows have are loaded; of kb >= kb1 nothing.
-  __device__ __forceinline__ void load(uint32_t lds, int kb, int st, int w, int i) const {
-    const uint32_t on = kb < kb1 ? ~0u : 0u;
-    if (i < kPieces) {
-      const uint32_t lo = kb < full ? on : on & (uint32_t)tail_lanes, hi = kb < full ? on : on & (uint32_t)(tail_lanes >> 32);
-      load16_to_lds((i < kPieces / 2 ? a_base : b_base) + (long long)kb * kBlock, off[i],
-                    lds + (uint32_t)(st * kStageBytes + (i * W + w) * 8 * kBlock), uniform64(lo, hi));
-    } else {
-      load4_to_lds(scale_base + (long long)kb * scale_ld, scale_at, lds + (uint32_t)(st * kStageBytes + kTileBytes + w * 256),
-                   uniform64(on, on));
-    }
-  }
-  __device__ __forceinline__ void load_all(uint32_t lds, int kb, int st, int w) const {
-#pragma unroll
-    for (int i = 0; i <= kPieces; ++i) load(lds, kb, st, w, i);
-  }
-};
-
-// Outputs y of row m, columns n to n + 3.
-template <class O, bool kVec>
-__device__ __forceinline__ void put4(const Fp8Product& p, int splits, int split, float* part, int m, int n, floatx4 y,
-                                     floatx4 bias) {
-  if (m >= p.M || n >= p.N) return;
-  if (splits > 1) finish4<float, kVec>(y, floatx4{}, false, part + ((long long)split * p.M + m) * p.N, n, p.N);
-  else finish4<O, kVec>(y, bias, p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
-}
-
-// The exact form: WM x WN waves of 32 x 32 tiles.
-template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kVec>
-__global__ void __launch_bounds__(64 * WM * WN, 2) matmul_exact_kernel(Fp8Product p, int tiles_m, int tiles_n, int splits,
-                                                                       int blocks_per_split, float* __restrict__ part) {
-  typedef Tile<BM, BN, WM * WN, kSquare> T;
-  constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
-  static_assert(BN / WN <= kBlock, "a wave's columns share a square block's scale");
-  __shared__ __attribute__((aligned(16))) char lds[2 * T::kStageBytes];
-  const uint32_t to = lds_address(lds);
-  const int lane = (int)lane_id();
-  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-  const int wm = w % WM, wn = w / WM;
-  const T tile(p, tiles_m, tiles_n, splits, blocks_per_split, w);
-  const int l32 = lane & 31, half = lane >> 5;
-  floatx16 acc[NT][MT] = {};
-  // Chunk 2 t + half of row r0 + l32: the same choice for a and b, so the lanes
-  // of a half hold the same k. Chunks past a row's end are zeros.
-  auto piece = [&](const char* stage, int r0, int t, int chunks) {
-    const intx4 v = *reinterpret_cast<const intx4*>(stage + (r0 + l32) * kBlock + (((2 * t + half) ^ swz(l32)) * 16));
-    return 2 * t + half < chunks ? v : intx4{};
-  };
-  auto block = [&](const char* stage, int chunks) {
-    const float* const sc = reinterpret_cast<const float*>(stage + T::kTileBytes);
-    float sa[MT];
-    Operands wa[MT][4];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      sa[i] = sc[(wm * MT + i) * 32 + l32];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) wa[i][t] = to_bf16(piece(stage, (wm * MT + i) * 32, t, chunks));
-    }
-    if constexpr (kSquare) {
-      const float sb = sc[BM + wn * NT * 32];
-#pragma unroll
-      for (int i = 0; i < MT; ++i) sa[i] *= sb;
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int r0 = BM + (wn * NT + j) * 32;
-      intx4 fb[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) fb[t] = piece(stage, r0, t, chunks);
-      floatx16 y[MT] = {};
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const Operands wb = to_bf16(fb[t]);
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int i = 0; i < MT; ++i)
-            y[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb.v[k], wa[i][t].v[k], y[i], 0, 0, 0);
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        floatx4 sb;
-        if constexpr (!kSquare) sb = *reinterpret_cast<const floatx4*>(sc + r0 + q * 8 + half * 4);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[j][i][4 * q + e] = fmaf(y[i][4 * q + e], kSquare ? sa[i] : sa[i] * sb[e], acc[j][i][4 * q + e]);
-      }
-    }
-  };
-  tile.load_all(to, tile.kb0, 0, w);
-  const int whole = min(tile.kb1, tile.full);
-  int st = 0;
-  for (int kb = tile.kb0; kb < whole; ++kb, st ^= 1) {
-    wait_all_loads();
-    barrier();                                           // this stage has landed; the other one is free
-    tile.load_all(to, kb + 1, st ^ 1, w);
-    block(lds + st * T::kStageBytes, 8);
-  }
-  if (whole < tile.kb1) {
-    wait_all_loads();
-    barrier();
-    block(lds + st * T::kStageBytes, tile.tail_chunks);
-  }
-#pragma unroll
-  for (int j = 0; j < NT; ++j)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int n = tile.n0 + (wn * NT + j) * 32 + q * 8 + half * 4;
-      const floatx4 bias = bias4<kVec>(p.bias, n, p.N);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-        put4<O, kVec>(p, splits, tile.split, part, tile.m0 + (wm * MT + i) * 32 + l32, n,
-                      floatx4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]}, bias);
-    }
-}
-
 // ---------------------------------------------------------------------------
-// The fast form: WM x WN waves of 16 x 16 tiles, one MFMA a tile and block.
-// A workgroup per CU walks a list of tiles, and its loads run on from one tile
-// to the next, so a tile's start waits for nothing and its outputs are written
-// while the next one's first blocks arrive.
-//
-// A group is one 16-row tile of b against the wave's MS tiles of a. While a
-// group's MFMAs run, the rows of b of the group after the next are read, and each
-// result is added up kBehind MFMAs later. The block's last two groups run behind the
-// barrier that frees the stage, tile of a by tile of a: a tile's registers take
-// its rows of the next stage as soon as its two MFMAs are issued, so the matrix
-// cores have work while the next block's first rows are read. The loads of the
-// block after that go out one by one, the first MS behind the barrier and the
-// others in the next block: as a burst of 9 they fill the address unit's queue,
-// and the waves wait there with their MFMAs behind.
+// The walk over the work. A workgroup's tiles are BM rows of a x BN rows of b; it
+// takes a list of them, and its loads run on from one tile to the next, so that a
+// tile's start waits for nothing and its outputs are written while the next one's
+// first blocks arrive.
 // ---------------------------------------------------------------------------
-constexpr int kBehind = 3;
-
 struct TileAt {
   int m0, n0, kb0, kb1, split;
 };
@@ -331,7 +135,7 @@ struct TileList {
 };
 // A block of a workgroup's list: block kb of a tile, `t` the tile's place. Workgroup
 // b runs on XCD b % 8, each XCD takes a run of the list, and its workgroups every
-// (gridDim / 8)th tile of the run: the 32 tiles that an XCD's CUs work on at a time
+// (gridDim / 8)th tile of the run: the tiles that an XCD's CUs work on at a time
 // are neighbours, whose rows its L2 holds.
 struct BlockAt {
   int t, end, kb;
@@ -340,10 +144,12 @@ struct BlockAt {
     const int run = (list.size() + 7) / 8, x = blockIdx.x % 8;
     t = x * run + (int)blockIdx.x / 8;
     end = min(x * run + run, list.size());
-    if (on()) tile = list.at(t), kb = tile.kb0;
+    kb = 0;
+    tile = on() ? list.at(t) : TileAt{};
+    kb = tile.kb0;
   }
   __device__ __forceinline__ bool on() const { return t < end; }
-  __device__ __forceinline__ void advance(const TileList& list) {   // true on a new tile
+  __device__ __forceinline__ void advance(const TileList& list) {
     if (on() && ++kb == tile.kb1) {
       t += (int)gridDim.x / 8;
       if (on()) tile = list.at(t), kb = tile.kb0;
@@ -351,70 +157,285 @@ struct BlockAt {
   }
 };
 
-template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kVec>
-__global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p, TileList list, float* __restrict__ part) {
-  constexpr int W = WM * WN;
-  constexpr int kTileBytes = (BM + BN) * kBlock, kStageBytes = kTileBytes + (BM + BN) * 4;
-  constexpr int MS = BM / WM / 16, NS = BN / WN / 16;
-  constexpr int kPieces = (BM + BN) / 8 / W;             // 8 rows x 128 bytes per load and wave: a's, then b's
-  constexpr int kMfmas = NS * MS, kLast = (NS - 2) * MS; // MFMAs of a block, and those before the barrier
-  constexpr int kEarly = kPieces / 2, kLate = kPieces - kEarly + 1;   // a's pieces behind the barrier; b's and the scales later,
-  constexpr int kGap = 2 * kLate <= kLast ? 2 : 1;       // every kGap MFMAs
+// The loads of W waves. Block n of the list goes to stage n % 2 of the LDS (rows of
+// a, then of b), its scales to place n % 4 behind the stages: a tile's last results
+// are added when the next block's scales are long there. While block n is worked
+// on, `late` is block n + 1 (its rows of b and its scales are loaded before the
+// barrier that ends the use of stage n) and `early` block n + 2 (its rows of a,
+// behind that barrier).
+template <int BM, int BN, int W, bool kSquare>
+struct Feed {
+  static constexpr int kStageBytes = (BM + BN) * kBlock, kScaleBytes = (BM + BN) * 4, kScales = 2 * kStageBytes;
+  static constexpr int kLds = kScales + 4 * kScaleBytes;
+  static constexpr int kPieces = (BM + BN) / 8 / W;      // 8 rows x 128 bytes per load and wave: a's, then b's
+  static constexpr int kEarly = kPieces / 2, kLate = kPieces - kEarly + 1;
   static_assert(BM == BN && kPieces == 8 && (BM + BN) / 64 == W, "four pieces of each operand and 64 scales a wave");
-  static_assert(kEarly == MS && kGap * kLate <= kLast, "a piece for every two MFMAs behind the barrier, the others before the next");
-  static_assert(kBehind <= MS && NS % 4 == 0, "a result is added up in the next group at the latest; the rings close with a block");
-  static_assert(BN / WN <= kBlock, "a wave's columns share a square block's scale");
-  __shared__ __attribute__((aligned(16))) char lds[2 * kStageBytes];
-  const uint32_t lds0 = lds_address(lds);
-  const int lane = (int)lane_id();
-  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-  const int wm = w % WM, wn = w / WM;
+  static_assert(W % 2 == 0, "pieces are 8 W rows apart, which keeps swz");
 
-  // ---- loads. Chunk (lane % 8) ^ swz(row) of 8 rows a piece; rows past the end
-  // read the last one, and their products are not stored. Of a block that is
-  // not whole only the chunks that the rows have are loaded, the others zeroed.
-  const int chunk = (lane % 8) ^ swz(w * 8 + lane / 8);  // the same in each piece: they are 8 W rows apart
-  static_assert(W % 2 == 0, "8 W rows apart keep swz");
-  const int full = p.K / kBlock;
-  const uint64_t tail_lanes = __ballot(chunk < p.K % kBlock / 16);
+  const Fp8Product& p;
+  const TileList& list;
+  char* const lds;
+  const uint32_t lds0;
+  const int w, lane, chunk;                              // chunk (lane % 8) ^ swz(row) of 8 rows a piece
+  const int full;                                        // whole blocks
+  const uint64_t tail_lanes;                             // the lanes whose chunks the block behind them has
+  const bool a_scale;
+  const float* const scale_base;
+  const int scale_ld;
   uint32_t off_a[kEarly], off_b[kPieces - kEarly], scale_at;
-  const bool a_scale = w * 64 < BM;
-  const float* const scale_base = a_scale ? p.a_scales : p.b_scales;
-  const int scale_ld = a_scale ? p.M : kSquare ? (p.N + kBlock - 1) / kBlock : p.N;
-  auto set_a = [&](const TileAt& t) {
+  BlockAt early, late;
+
+  __device__ __forceinline__ Feed(const Fp8Product& p_, const TileList& list_, char* lds_, int w_)
+      : p(p_), list(list_), lds(lds_), lds0(lds_address(lds_)), w(w_), lane((int)lane_id()),
+        chunk((lane % 8) ^ swz(w * 8 + lane / 8)), full(p_.K / kBlock),
+        tail_lanes(__ballot(chunk < p_.K % kBlock / 16)), a_scale(w * 64 < BM),
+        scale_base(a_scale ? p_.a_scales : p_.b_scales),
+        scale_ld(a_scale ? p_.M : kSquare ? (p_.N + kBlock - 1) / kBlock : p_.N), early(list_), late(early) {}
+
+  // Rows past the end read the last one; their products are not stored.
+  __device__ __forceinline__ void set_a(const TileAt& t) {
 #pragma unroll
     for (int i = 0; i < kEarly; ++i)
       off_a[i] = (uint32_t)min((i * W + w) * 8 + lane / 8, p.M - 1 - t.m0) * (uint32_t)p.K + (uint32_t)chunk * 16u;
-  };
-  auto set_b = [&](const TileAt& t) {
+  }
+  __device__ __forceinline__ void set_b(const TileAt& t) {
 #pragma unroll
     for (int i = 0; i < kPieces - kEarly; ++i)
       off_b[i] = (uint32_t)min((i * W + w) * 8 + lane / 8, p.N - 1 - t.n0) * (uint32_t)p.K + (uint32_t)chunk * 16u;
     const int r = w * 64 + lane, n = min(t.n0 + r - BM, p.N - 1);
     scale_at = (uint32_t)(a_scale ? min(t.m0 + r, p.M - 1) : kSquare ? n / kBlock : n) * 4u;
-  };
-  auto load = [&](const BlockAt& at, int st, int i) {    // piece i of a block, kPieces: its scales
-    const uint32_t on = at.on() ? ~0u : 0u;
-    const uint32_t stage = lds0 + (uint32_t)(st * kStageBytes);
-    if (i < kPieces) {
-      const uint32_t lo = at.kb < full ? on : on & (uint32_t)tail_lanes, hi = at.kb < full ? on : on & (uint32_t)(tail_lanes >> 32);
-      const uint64_t mask = uniform64(lo, hi);
-      const char* base = reinterpret_cast<const char*>(i < kEarly ? p.a : p.b) +
-                         (long long)(i < kEarly ? at.tile.m0 : at.tile.n0) * p.K + (long long)at.kb * kBlock;
-      load16_to_lds(base, i < kEarly ? off_a[i < kEarly ? i : 0] : off_b[i < kEarly ? 0 : i - kEarly],
-                    stage + (uint32_t)((i * W + w) * 8 * kBlock), mask);
+  }
+  // All ones where x < y. Masks by scalar arithmetic: written as comparisons and
+  // choices they go through the vector ALU and back, 36 of its instructions a block.
+  static __device__ __forceinline__ uint32_t below(int x, int y) {
+    uint32_t m;
+    asm("s_sub_i32 %0, %1, %2\n\ts_ashr_i32 %0, %0, 31" : "=s"(m) : "s"(x), "s"(y) : "scc");
+    return m;
+  }
+  __device__ __forceinline__ uint64_t mask(const BlockAt& at) const {
+    const uint32_t on = below(at.t, at.end), whole = below(at.kb, full);
+    return (uint64_t)(on & (whole | (uint32_t)(tail_lanes >> 32))) << 32 | (on & (whole | (uint32_t)tail_lanes));
+  }
+  __device__ __forceinline__ void load_a(const BlockAt& at, int n, int i) const {
+    load16_to_lds(reinterpret_cast<const char*>(p.a) + (long long)at.tile.m0 * p.K + (long long)at.kb * kBlock, off_a[i],
+                  lds0 + (uint32_t)((n & 1) * kStageBytes + (i * W + w) * 8 * kBlock), mask(at));
+  }
+  __device__ __forceinline__ void load_b(const BlockAt& at, int n, int i) const {   // i = kLate - 1: the scales
+    if (i < kLate - 1) {
+      load16_to_lds(reinterpret_cast<const char*>(p.b) + (long long)at.tile.n0 * p.K + (long long)at.kb * kBlock, off_b[i],
+                    lds0 + (uint32_t)((n & 1) * kStageBytes + ((i + kEarly) * W + w) * 8 * kBlock), mask(at));
     } else {
-      load4_to_lds(scale_base + (long long)at.kb * scale_ld, scale_at, stage + (uint32_t)(kTileBytes + w * 256), uniform64(on, on));
+      const uint32_t on = below(at.t, at.end);
+      load4_to_lds(scale_base + (long long)at.kb * scale_ld, scale_at,
+                   lds0 + (uint32_t)(kScales + (n & 3) * kScaleBytes + w * 256), (uint64_t)on << 32 | on);
     }
-  };
-  // The zeros of a block that is not whole (in its own branch: one block in a tile at most).
-  auto zero_tail = [&](const BlockAt& at, int st, int first, int last) {
+  }
+  // Of a block that is not whole the chunks past the rows' end: zeros.
+  __device__ __forceinline__ void zero_tail(const BlockAt& at, int n, int first, int last) const {
     if (!at.on() || at.kb < full || chunk * 16 < p.K % kBlock) return;
     for (int i = first; i < last; ++i)
-      *reinterpret_cast<intx4*>(lds + st * kStageBytes + (i * W + w) * 8 * kBlock + lane * 16) = intx4{};
+      *reinterpret_cast<intx4*>(lds + (n & 1) * kStageBytes + (i * W + w) * 8 * kBlock + lane * 16) = intx4{};
+  }
+  // Block 0 whole, and the rows of a of block 1; early is then block 1.
+  __device__ __forceinline__ void start() {
+    set_a(early.tile);
+    set_b(early.tile);
+#pragma unroll
+    for (int i = 0; i < kEarly; ++i) load_a(early, 0, i);
+#pragma unroll
+    for (int i = 0; i < kLate; ++i) load_b(early, 0, i);
+    zero_tail(early, 0, 0, kPieces);
+    wait_all_loads();
+    barrier();
+    early.advance(list);
+    if (early.on() && early.t != late.t) set_a(early.tile);
+#pragma unroll
+    for (int i = 0; i < kEarly; ++i) load_a(early, 1, i);
+    zero_tail(early, 1, 0, kEarly);
+  }
+  // On to block n.
+  __device__ __forceinline__ void next(int n) {
+    if (early.on() && early.t != late.t) set_b(early.tile);
+    late = early;
+    early.advance(list);
+    if (early.on() && early.t != late.t) set_a(early.tile);
+    zero_tail(late, n + 1, kEarly, kPieces);
+  }
+  __device__ __forceinline__ void late_piece(int n, int i) const { load_b(late, n + 1, i); }
+  __device__ __forceinline__ void early_piece(int n, int i) const { load_a(early, n, i); }
+  __device__ __forceinline__ void end_block(int n) const { zero_tail(early, n, 0, kEarly); }
+  __device__ __forceinline__ const char* stage(int n) const { return lds + (n & 1) * kStageBytes; }
+  __device__ __forceinline__ const char* scales(int n) const { return lds + kScales + (n & 3) * kScaleBytes; }
+};
+
+// Outputs y of row m, columns n to n + 3.
+template <class O, bool kVec>
+__device__ __forceinline__ void put4(const Fp8Product& p, int splits, int split, float* part, int m, int n, floatx4 y,
+                                     floatx4 bias) {
+  if (m >= p.M || n >= p.N) return;
+  if (splits > 1) finish4<float, kVec>(y, floatx4{}, false, part + ((long long)split * p.M + m) * p.N, n, p.N);
+  else finish4<O, kVec>(y, bias, p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
+}
+
+// ---------------------------------------------------------------------------
+// The exact form: 2 x 2 waves, each of 2 x 2 tiles of 32 x 32, in the order (tile
+// of b, tile of a). A tile's block is a chain of 8 MFMAs; beside each go its share of
+// the last chain's 16 additions and of the conversions to bf16: of b's next rows
+// into the registers that a chain against a's second tile has used, and of a's
+// next rows into those that b's second tile has. Per MFMA (32 cycles) that is 4
+// conversions, 2 additions and, with a scale per row of b, 2 products: 24 to 32
+// cycles of the vector ALU, so the two workgroups of a CU keep both busy.
+// ---------------------------------------------------------------------------
+template <bool kSquare, class O, bool kVec>
+__global__ void __launch_bounds__(256, 2) matmul_exact_kernel(Fp8Product p, TileList list, float* __restrict__ part) {
+  constexpr int BM = 128, BN = 128, WM = 2;
+  typedef Feed<BM, BN, 4, kSquare> F;
+  __shared__ __attribute__((aligned(16))) char lds[F::kLds];
+  const int lane = (int)lane_id();
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const int wm = w % WM, wn = w / WM;
+  const int l32 = lane & 31, half = lane >> 5;
+  const int at_a = (wm * 64 + l32) * kBlock, at_b = (BM + wn * 64 + l32) * kBlock;
+  // Chunk 2 t + half of a row: the same choice for a and b, so the lanes of a half
+  // hold the same k.
+  auto piece = [&](const char* stage, int at, int t) {
+    return *reinterpret_cast<const intx4*>(stage + at + (((2 * t + half) ^ swz(l32)) * 16));
+  };
+  floatx16 acc[2][2], y[2];                              // y[c % 2]: of chain c = (tile of b, tile of a)
+  Operands wa[2][4], wb[4];
+  float sa[2], sa_next[2];
+  auto pin = [](Operands& o) { asm volatile("" : "+v"(o.v[0]), "+v"(o.v[1])); };
+  auto read_scales = [&](const char* scales) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      sa_next[i] = *reinterpret_cast<const float*>(scales + (wm * 64 + i * 32 + l32) * 4);
+      if constexpr (kSquare) sa_next[i] *= *reinterpret_cast<const float*>(scales + (BM + wn * 64) * 4);
+    }
+  };
+  // Quad q of chain c's results, with the scales of its block.
+  auto add_up = [&](const char* scales, const float (&s)[2], int c, int q) {
+    const int j = c / 2, i = c % 2;
+    floatx4 sb;
+    if constexpr (!kSquare)
+      sb = *reinterpret_cast<const floatx4*>(scales + (BM + wn * 64 + j * 32 + 8 * q + 4 * half) * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc[j][i][4 * q + e] = fmaf(y[c % 2][4 * q + e], kSquare ? s[i] : s[i] * sb[e], acc[j][i][4 * q + e]);
+    asm volatile("" : "+v"(acc[j][i]));                  // here, and not behind the block (see the fast form)
   };
 
-  // ---- fragments and sums
+  F feed(p, list, lds, w);
+  BlockAt cur = feed.early;
+  if (!cur.on()) return;
+  feed.start();
+  intx4 raw_a[2], raw_b[2];                              // pieces read and not yet converted
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    wb[t] = to_bf16(piece(feed.stage(0), at_b, t));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) wa[i][t] = to_bf16(piece(feed.stage(0), at_a + i * 32 * kBlock, t));
+  }
+  raw_b[1] = piece(feed.stage(0), at_b, 3);              // as the block before would have left them
+  raw_a[1] = piece(feed.stage(0), at_a + 32 * kBlock, 3);
+  read_scales(feed.scales(0));
+
+  for (int n = 0; cur.on();) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[j][i] = floatx16{};
+    for (; cur.kb < cur.tile.kb1; ++cur.kb, ++n) {
+      feed.next(n);
+      const char *const stage = feed.stage(n), *const next = feed.stage(n + 1), *const scales = feed.scales(n);
+      sa[0] = sa_next[0], sa[1] = sa_next[1];
+      // MFMA s of chain c, and what goes beside it. A piece is read at an even s and
+      // converted three MFMAs later, at the earliest behind the last MFMA that uses
+      // the registers it goes to; past the list's end it is stale, and never used.
+      auto step = [&](int c, int s) {
+        const int i = c % 2, t = s / 2;
+        y[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[t].v[s % 2], wa[i][t].v[s % 2], s ? y[i] : floatx16{}, 0, 0, 0);
+        asm volatile("" : "+v"(y[i]));
+        if (s % 2 == 0) {
+          if (c == 1) raw_b[t % 2] = piece(stage, at_b + 32 * kBlock, t);
+          if (c == 3) raw_b[t % 2] = piece(next, at_b, t);
+          if (c >= 2) raw_a[t % 2] = piece(next, at_a + i * 32 * kBlock, t);
+        } else {
+          const int from = s == 1 ? (c + 3) % 4 : c, u = s == 1 ? 3 : t - 1;   // piece u that chain `from` has read
+          if (from % 2 == 1) {
+            wb[u] = to_bf16(raw_b[u % 2]);
+            pin(wb[u]);
+          }
+          if (from >= 2) {
+            wa[from % 2][u] = to_bf16(raw_a[u % 2]);
+            pin(wa[from % 2][u]);
+          }
+          if (c > 0) add_up(scales, sa, c - 1, t);
+          const int k = c * 4 + t;                       // the loads: one every two MFMAs
+          if (k < F::kLate) feed.late_piece(n, k);
+          if (c >= 2 && k - 8 < F::kEarly) feed.early_piece(n, k - 8);
+        }
+        __builtin_amdgcn_sched_barrier(0);               // in this order: the compiler's own waits for each result
+      };
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) step(c, s);
+      wait_all_loads();
+      barrier();                                         // the next stage has landed, this one is free
+#pragma unroll
+      for (int c = 2; c < 4; ++c)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) step(c, s);
+      read_scales(feed.scales(n + 1));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) add_up(scales, sa, 3, q);
+      feed.end_block(n);
+    }
+    const TileAt done = cur.tile;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = done.n0 + wn * 64 + j * 32 + q * 8 + half * 4;
+        const floatx4 bias = bias4<kVec>(p.bias, col, p.N);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          put4<O, kVec>(p, list.splits, done.split, part, done.m0 + wm * 64 + i * 32 + l32, col,
+                        floatx4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]}, bias);
+      }
+    cur.kb = cur.tile.kb1 - 1;
+    cur.advance(list);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The fast form: WM x WN waves of 16 x 16 tiles, one MFMA a tile and block.
+// A group is one 16-row tile of b against the wave's MS tiles of a. While a
+// group's MFMAs run, the rows of b of the group after the next are read, and each
+// result is added up kBehind MFMAs later. The block's last two groups run behind the
+// barrier that frees the stage, tile of a by tile of a: a tile's registers take
+// its rows of the next stage as soon as its two MFMAs are issued, so the matrix
+// cores have work while the next block's first rows are read. The loads of the
+// block after that go out one by one, the first MS behind the barrier and the
+// others in the next block: as a burst of 9 they fill the address unit's queue,
+// and the waves wait there with their MFMAs behind.
+// ---------------------------------------------------------------------------
+constexpr int kBehind = 3;
+
+template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kVec>
+__global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p, TileList list, float* __restrict__ part) {
+  typedef Feed<BM, BN, WM * WN, kSquare> F;
+  constexpr int MS = BM / WM / 16, NS = BN / WN / 16;
+  constexpr int kMfmas = NS * MS, kLast = (NS - 2) * MS; // MFMAs of a block, and those before the barrier
+  constexpr int kGap = 2 * F::kLate <= kLast ? 2 : 1;    // between the late pieces
+  static_assert(F::kEarly == MS && kGap * F::kLate <= kLast, "a piece for every two MFMAs behind the barrier, the others before the next");
+  static_assert(kBehind <= MS && NS % 4 == 0, "a result is added up in the next group at the latest; the rings close with a block");
+  static_assert(BN / WN <= kBlock, "a wave's columns share a square block's scale");
+  __shared__ __attribute__((aligned(16))) char lds[F::kLds];
+  const int lane = (int)lane_id();
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const int wm = w % WM, wn = w / WM;
+
   const int l16 = lane & 15, g4 = lane >> 4;
   const int at_a = (wm * MS * 16 + l16) * kBlock, at_b = (BM + wn * NS * 16 + l16) * kBlock;
   const int lo = (g4 ^ swz(l16)) * 16, hi = ((g4 + 4) ^ swz(l16)) * 16;   // chunks g4 and g4 + 4 of a row
@@ -427,16 +448,16 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
   float sa[MS], sa_next[MS];
   floatx4 sb[4];
   floatx4 y[kBehind + 1];
-  const int at_sa = kTileBytes + (wm * MS * 16 + l16) * 4, at_sb = kTileBytes + (BM + wn * NS * 16) * 4;
-  auto read_b = [&](const char* stage, int j) {
+  const int at_sa = (wm * MS * 16 + l16) * 4, at_sb = (BM + wn * NS * 16) * 4;
+  auto read_b = [&](const char* stage, const char* scales, int j) {
     fb[j % 4] = rows(stage, at_b + j * 16 * kBlock);
-    if constexpr (!kSquare) sb[j % 4] = *reinterpret_cast<const floatx4*>(stage + at_sb + j * 64 + g4 * 16);
+    if constexpr (!kSquare) sb[j % 4] = *reinterpret_cast<const floatx4*>(scales + at_sb + j * 64 + g4 * 16);
   };
-  auto read_scales = [&](const char* stage) {
+  auto read_scales = [&](const char* scales) {
 #pragma unroll
     for (int i = 0; i < MS; ++i) {
-      sa_next[i] = *reinterpret_cast<const float*>(stage + at_sa + i * 64);
-      if constexpr (kSquare) sa_next[i] *= *reinterpret_cast<const float*>(stage + at_sb);
+      sa_next[i] = *reinterpret_cast<const float*>(scales + at_sa + i * 64);
+      if constexpr (kSquare) sa_next[i] *= *reinterpret_cast<const float*>(scales + at_sb);
     }
   };
   // MFMA number t of a block is of this group and tile of a: the last two groups in the order of a's tiles.
@@ -457,53 +478,36 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
     asm volatile("" : "+v"(acc[j][i]));
   };
 
-  BlockAt cur(list);
+  F feed(p, list, lds, w);
+  BlockAt cur = feed.early;
   if (!cur.on()) return;
-  BlockAt early = cur, late = cur;
-  set_a(cur.tile);
-  set_b(cur.tile);
+  feed.start();
+  read_b(feed.stage(0), feed.scales(0), 0);
+  read_b(feed.stage(0), feed.scales(0), 1);
 #pragma unroll
-  for (int i = 0; i <= kPieces; ++i) load(cur, 0, i);
-  zero_tail(cur, 0, 0, kPieces);
-  wait_all_loads();
-  barrier();
-  early.advance(list);
-  if (early.on() && early.t != cur.t) set_a(early.tile);
-#pragma unroll
-  for (int i = 0; i < kEarly; ++i) load(early, 1, i);
-  zero_tail(early, 1, 0, kEarly);
-  read_b(lds, 0);
-  read_b(lds, 1);
-#pragma unroll
-  for (int i = 0; i < MS; ++i) fa[i] = rows(lds, at_a + i * 16 * kBlock);
-  read_scales(lds);
+  for (int i = 0; i < MS; ++i) fa[i] = rows(feed.stage(0), at_a + i * 16 * kBlock);
+  read_scales(feed.scales(0));
 
-  for (int st = 0; cur.on();) {
+  for (int n = 0; cur.on();) {
 #pragma unroll
     for (int j = 0; j < NS; ++j)
 #pragma unroll
       for (int i = 0; i < MS; ++i) acc[j][i] = floatx4{};
-    for (; cur.kb < cur.tile.kb1; ++cur.kb, st ^= 1) {
-      // This block is in stage st; late, the next one, goes to the other stage, and
-      // early, the one after that, to this one.
-      if (early.on() && early.t != late.t) set_b(early.tile);
-      late = early;
-      early.advance(list);
-      if (early.on() && early.t != late.t) set_a(early.tile);
-      zero_tail(late, st ^ 1, kEarly, kPieces);
-      const char* const stage = lds + st * kStageBytes;
-      const char* const next = lds + (st ^ 1) * kStageBytes;
+    for (; cur.kb < cur.tile.kb1; ++cur.kb, ++n) {
+      feed.next(n);
+      const char *const stage = feed.stage(n), *const next = feed.stage(n + 1);
+      const char *const scales = feed.scales(n), *const next_scales = feed.scales(n + 1);
 #pragma unroll
       for (int i = 0; i < MS; ++i) sa[i] = sa_next[i];
 #pragma unroll
       for (int j = 0; j < NS - 2; ++j) {
-        read_b(stage, j + 2);
+        read_b(stage, scales, j + 2);
         __builtin_amdgcn_sched_barrier(0);               // in this order: the compiler's own waits for each result
 #pragma unroll
         for (int t = j * MS; t < (j + 1) * MS; ++t) {
           multiply(t);
           if (t >= kBehind) add_up(t - kBehind);
-          if (t % kGap == kGap - 1 && t / kGap < kLate) load(late, st ^ 1, kEarly + t / kGap);
+          if (t % kGap == kGap - 1 && t / kGap < F::kLate) feed.late_piece(n, t / kGap);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -513,16 +517,16 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
       for (int t = kLast; t < kMfmas; ++t) {             // past the list's end the reads are of a stale stage, never used
         multiply(t);
         add_up(t - kBehind);
-        if (t == kLast) read_b(next, 0);
-        if (t == kLast + kBehind) read_b(next, 1);       // its scales' registers: group NS - 3's last result is added
-        if (t % 2 == 0) load(early, st, (t - kLast) / 2);
+        if (t == kLast) read_b(next, next_scales, 0);
+        if (t == kLast + kBehind) read_b(next, next_scales, 1);   // its scales' registers: group NS - 3's last result is added
+        if (t % 2 == 0) feed.early_piece(n, (t - kLast) / 2);
         if ((t - kLast) % 2) fa[of_a(t)] = rows(next, at_a + of_a(t) * 16 * kBlock);
         __builtin_amdgcn_sched_barrier(0);
       }
-      read_scales(next);
+      read_scales(next_scales);
 #pragma unroll
       for (int t = kMfmas - kBehind; t < kMfmas; ++t) add_up(t);
-      zero_tail(early, st, 0, kEarly);
+      feed.end_block(n);
     }
     const TileAt done = cur.tile;
     const bool octets = sizeof(O) == 2 && p.N % 8 == 0 && list.splits == 1;
@@ -581,25 +585,27 @@ Plan plan_matmul(int M, int N, int K, bool fast) {
   pl.tile = fast && big >= 192 ? 256 : 128;
   const long long tiles = (long long)ceil_div(M, pl.tile) * ceil_div(N, pl.tile);
   int splits = 1;
-  while (tiles * splits < 192 && kb / (splits * 2) >= 4) splits *= 2;
+  while (tiles * splits <= 256 && kb / (splits * 2) >= 4) splits *= 2;
   pl.blocks_per_split = ceil_div(kb, splits);
   pl.splits = ceil_div(kb, pl.blocks_per_split);
   return pl;
 }
 
-template <int BM, int BN, int WM, int WN, bool kFast, bool kSquare, class O, bool kVec>
+// Workgroups: as many as the chip holds at a time, by their LDS, or one per tile.
+unsigned grid_of(const TileList& list) {
+  return std::min(((unsigned)list.size() + 7) / 8 * 8, list.bm == 256 ? 256u : 512u);
+}
+
+template <bool kSquare, class O, bool kVec>
 hipError_t run_tiles(const Fp8Product& p, const Plan& pl, float* part, hipStream_t stream) {
-  const int tiles_m = ceil_div(p.M, BM), tiles_n = ceil_div(p.N, BN);
+  const TileList list{ceil_div(p.M, pl.tile), ceil_div(p.N, pl.tile), pl.splits, pl.blocks_per_split, ceil_div(p.K, kBlock),
+                      pl.tile, pl.tile};
+  const unsigned grid = grid_of(list);
   {
-    LaunchScope scope(kFast ? "matmul_fast_kernel" : "matmul_exact_kernel", stream);
-    const unsigned grid = (unsigned)(tiles_m * tiles_n * pl.splits);
-    if constexpr (kFast) {
-      const TileList list{tiles_m, tiles_n, pl.splits, pl.blocks_per_split, ceil_div(p.K, kBlock), BM, BN};
-      const unsigned most = BM == 256 ? 256 : 512;       // workgroups that the chip holds at a time (by their LDS)
-      matmul_fast_kernel<BM, BN, WM, WN, kSquare, O, kVec><<<std::min((grid + 7) / 8 * 8, most), 64 * WM * WN, 0, stream>>>(p, list, part);
-    } else
-      matmul_exact_kernel<BM, BN, WM, WN, kSquare, O, kVec><<<grid, 64 * WM * WN, 0, stream>>>(
-          p, tiles_m, tiles_n, pl.splits, pl.blocks_per_split, part);
+    LaunchScope scope(p.fast ? "matmul_fast_kernel" : "matmul_exact_kernel", stream);
+    if (pl.tile == 256) matmul_fast_kernel<256, 256, 4, 2, kSquare, O, kVec><<<grid, 512, 0, stream>>>(p, list, part);
+    else if (p.fast) matmul_fast_kernel<128, 128, 2, 2, kSquare, O, kVec><<<grid, 256, 0, stream>>>(p, list, part);
+    else matmul_exact_kernel<kSquare, O, kVec><<<grid, 256, 0, stream>>>(p, list, part);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1) return e;
   }
@@ -609,16 +615,10 @@ hipError_t run_tiles(const Fp8Product& p, const Plan& pl, float* part, hipStream
   return hipGetLastError();
 }
 
-template <bool kSquare, class O, bool kVec>
-hipError_t run_by_tile(const Fp8Product& p, float* part, hipStream_t stream) {
-  const Plan pl = plan_matmul(p.M, p.N, p.K, p.fast);
-  if (pl.tile == 256) return run_tiles<256, 256, 4, 2, true, kSquare, O, kVec>(p, pl, part, stream);
-  return p.fast ? run_tiles<128, 128, 2, 2, true, kSquare, O, kVec>(p, pl, part, stream)
-                : run_tiles<128, 128, 2, 2, false, kSquare, O, kVec>(p, pl, part, stream);
-}
 template <bool kSquare, class O>
 hipError_t run_by_alignment(const Fp8Product& p, float* part, hipStream_t stream) {
-  return p.N % 4 == 0 ? run_by_tile<kSquare, O, true>(p, part, stream) : run_by_tile<kSquare, O, false>(p, part, stream);
+  const Plan pl = plan_matmul(p.M, p.N, p.K, p.fast);
+  return p.N % 4 == 0 ? run_tiles<kSquare, O, true>(p, pl, part, stream) : run_tiles<kSquare, O, false>(p, pl, part, stream);
 }
 
 }  // namespace
