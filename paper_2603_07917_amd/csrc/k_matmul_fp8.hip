@@ -557,6 +557,79 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
   }
 }
 
+// ---------------------------------------------------------------------------
+// Few rows of a (one decision's prompts): bound by the one pass over b. A workgroup
+// takes 16 rows of b and all of a's, each of its waves every 8th block of the sum,
+// straight into registers; the waves' sums meet in LDS. The sums are exact in
+// either form: the matrix cores wait for the memory here.
+// ---------------------------------------------------------------------------
+constexpr int kFewRows = 64, kFewWaves = 8;
+
+template <int MT, bool kSquare, class O, bool kVec>
+__global__ void __launch_bounds__(64 * kFewWaves) matmul_few_kernel(Fp8Product p) {
+  __shared__ floatx4 sums[kFewWaves - 1][MT][64];
+  const int lane = (int)lane_id(), w = threadIdx.x / 64;
+  const int l16 = lane & 15, g4 = lane >> 4;
+  const int n0 = blockIdx.x * 16, kblocks = (p.K + kBlock - 1) / kBlock;
+  const uint8_t* const row_b = p.b + (long long)min(n0 + l16, p.N - 1) * p.K;   // rows past the end are not stored
+  const uint8_t* row_a[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) row_a[i] = p.a + (long long)min(i * 16 + l16, p.M - 1) * p.K;
+  const int blocks_n = (p.N + kBlock - 1) / kBlock;
+  auto chunk = [&](const uint8_t* row, int kb, int c) {  // 16 bytes, zeros past the row's end
+    const int at = kb * kBlock + c * 16;
+    return at < p.K ? *reinterpret_cast<const intx4*>(row + at) : intx4{};
+  };
+  floatx4 acc[MT] = {};
+#pragma unroll 2
+  for (int kb = w; kb < kblocks; kb += kFewWaves) {
+    intx4 b[2], a[MT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                        // chunks g4 and g4 + 4: the same choice for a and b
+      b[h] = chunk(row_b, kb, g4 + 4 * h);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[i][h] = chunk(row_a[i], kb, g4 + 4 * h);
+    }
+    floatx4 sb;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      sb[e] = kSquare ? p.b_scales[(long long)kb * blocks_n + n0 / kBlock]
+                      : p.b_scales[(long long)kb * p.N + min(n0 + 4 * g4 + e, p.N - 1)];
+    float sa[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sa[i] = p.a_scales[(long long)kb * p.M + min(i * 16 + l16, p.M - 1)];
+    floatx4 y[MT] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const Operands wb = to_bf16(b[h]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const Operands wa = to_bf16(a[i][h]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) y[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb.v[k], wa.v[k], y[i], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(y[i][e], sa[i] * sb[e], acc[i][e]);
+  }
+  if (w > 0) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sums[w - 1][i][lane] = acc[i];
+  }
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    floatx4 y = acc[i];
+#pragma unroll
+    for (int k = 0; k < kFewWaves - 1; ++k) y += sums[k][i][lane];
+    const int m = i * 16 + l16, n = n0 + 4 * g4;
+    put4<O, kVec>(p, 1, 0, nullptr, m, n, y, bias4<kVec>(p.bias, n, p.N));
+  }
+}
+
 // The splits' sums, in order.
 template <class O, bool kVec>
 __global__ void __launch_bounds__(256) matmul_join_kernel(Fp8Product p, int splits, const float* __restrict__ part) {
@@ -575,12 +648,13 @@ __global__ void __launch_bounds__(256) matmul_join_kernel(Fp8Product p, int spli
 }
 
 struct Plan {
-  int tile;                  // rows of a and of b per workgroup
+  int tile;                  // rows of a and of b per workgroup, 0: few rows
   int splits, blocks_per_split;
 };
 Plan plan_matmul(int M, int N, int K, bool fast) {
   Plan pl;
   const int kb = ceil_div(K, kBlock);
+  if (M <= kFewRows) return Plan{0, 1, kb};
   const long long big = (long long)ceil_div(M, 256) * ceil_div(N, 256);
   pl.tile = fast && big >= 192 ? 256 : 128;
   const long long tiles = (long long)ceil_div(M, pl.tile) * ceil_div(N, pl.tile);
@@ -598,6 +672,14 @@ unsigned grid_of(const TileList& list) {
 
 template <bool kSquare, class O, bool kVec>
 hipError_t run_tiles(const Fp8Product& p, const Plan& pl, float* part, hipStream_t stream) {
+  if (pl.tile == 0) {
+    LaunchScope scope("matmul_few_kernel", stream);
+    const unsigned grid = (unsigned)ceil_div(p.N, 16);
+    if (p.M <= 16) matmul_few_kernel<1, kSquare, O, kVec><<<grid, 64 * kFewWaves, 0, stream>>>(p);
+    else if (p.M <= 32) matmul_few_kernel<2, kSquare, O, kVec><<<grid, 64 * kFewWaves, 0, stream>>>(p);
+    else matmul_few_kernel<4, kSquare, O, kVec><<<grid, 64 * kFewWaves, 0, stream>>>(p);
+    return hipGetLastError();
+  }
   const TileList list{ceil_div(p.M, pl.tile), ceil_div(p.N, pl.tile), pl.splits, pl.blocks_per_split, ceil_div(p.K, kBlock),
                       pl.tile, pl.tile};
   const unsigned grid = grid_of(list);

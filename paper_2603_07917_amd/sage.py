@@ -502,9 +502,10 @@ def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> to
     return t
 
 
-def _result(out: Optional[torch.Tensor], shape, dtype, device, name: str = "out") -> torch.Tensor:
+def _result(out: Optional[torch.Tensor], shape, dtype, like: torch.Tensor, name: str = "out") -> torch.Tensor:
+    """`out` checked, or a new tensor on `like`'s device."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     _dev(out, dtype, name, len(shape))
     if tuple(out.shape) != tuple(shape):
         raise SageError(f"{name} must be {tuple(shape)}, got {tuple(out.shape)}")
@@ -544,7 +545,7 @@ def embed(tokens: torch.Tensor, table: torch.Tensor, scale: float = 1.0, offsets
     dtype = dtype or (table.dtype if out is None else out.dtype)
     if dtype not in _ROW_TYPES:
         raise SageError("dtype must be float32 or bfloat16")
-    out = _result(out, (T if offsets is None else Q, d), dtype, table.device)
+    out = _result(out, (T if offsets is None else Q, d), dtype, table)
     lib = load_library()
     ws = _scratch(workspace, 0 if offsets is None else lib.sage_embed_workspace_bytes(T, Q, d), table.device)
     _check(lib.sage_embed(_ptr(tokens), T, _ptr(table), TYPES[table.dtype], V, d, float(scale), _ptr(offsets), Q,
@@ -567,7 +568,7 @@ def embed_grad(tokens: torch.Tensor, grad: torch.Tensor, vocab: int, scale: floa
         _dev(add, torch.float32, "add", 2)
         if tuple(add.shape) != (V, d):
             raise SageError(f"add must be {(V, d)}, got {tuple(add.shape)}")
-    out = _result(out, (V, d), torch.float32, grad.device)
+    out = _result(out, (V, d), torch.float32, grad)
     lib = load_library()
     ws = _scratch(workspace, lib.sage_embed_grad_workspace_bytes(T, Q, V, d), grad.device)
     _check(lib.sage_embed_grad(_ptr(tokens), T, _ptr(grad), TYPES[grad.dtype], V, d, float(scale), _ptr(offsets), Q,
@@ -599,10 +600,10 @@ def rms_norm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tenso
     if dtype not in TYPES:
         raise SageError("dtype must be float32, bfloat16 or float8_e4m3fn")
     fp8 = dtype == torch.float8_e4m3fn
-    out = _result(out, (M, -(-d // 16) * 16 if fp8 else d), dtype, x.device)
-    scales = _result(scales, _scale_shape(M, d, "row"), torch.float32, x.device, "scales") if fp8 else None
+    out = _result(out, (M, -(-d // 16) * 16 if fp8 else d), dtype, x)
+    scales = _result(scales, _scale_shape(M, d, "row"), torch.float32, x, "scales") if fp8 else None
     if total is not None or residual is not None:
-        total = _result(total, (M, d), x.dtype, x.device, "total")
+        total = torch.empty_like(x) if total is None else _result(total, (M, d), x.dtype, x, "total")
     _check(load_library().sage_rms_norm(_ptr(x), _ptr(residual), TYPES[x.dtype], M, d, _ptr(gain), float(eps),
                                         _ptr(total), _ptr(out), TYPES[dtype], _ptr(scales), _stream()))
     return out, scales, total
@@ -622,7 +623,7 @@ def rms_norm_grad(grad: torch.Tensor, total: torch.Tensor, gain: torch.Tensor, e
         raise SageError("gain must have one entry per column")
     if grad_total is not None:
         _rows(grad_total, "grad_total", total)
-    out = _result(out, (M, d), total.dtype, total.device)
+    out = torch.empty_like(total) if out is None else _result(out, (M, d), total.dtype, total)
     grad_gain = torch.empty(d, dtype=torch.float32, device=total.device)
     lib = load_library()
     ws = _scratch(workspace, lib.sage_rms_norm_grad_workspace_bytes(M, d), total.device)
@@ -640,8 +641,8 @@ def quantize(x: torch.Tensor, block: str = "row", transpose: bool = False, out: 
         raise SageError(f"unknown block {block!r}")
     M, K = x.shape
     R, C = (K, M) if transpose else (M, K)
-    out = _result(out, (R, -(-C // 16) * 16), torch.float8_e4m3fn, x.device)
-    scales = _result(scales, _scale_shape(R, C, block), torch.float32, x.device, "scales")
+    out = _result(out, (R, -(-C // 16) * 16), torch.float8_e4m3fn, x)
+    scales = _result(scales, _scale_shape(R, C, block), torch.float32, x, "scales")
     _check(load_library().sage_quantize(_ptr(x), TYPES[x.dtype], M, K, BLOCKS[block], int(bool(transpose)), _ptr(out),
                                         _ptr(scales), _stream()))
     return out, scales
@@ -663,12 +664,12 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     (M, K), N = a.shape, b.shape[0]
     if b.shape[1] != K:
         raise SageError("a and b must have rows of one length")
-    if tuple(a_scales.shape) != _scale_shape(M, K, "row"):
-        raise SageError(f"a_scales must be {_scale_shape(M, K, 'row')}, got {tuple(a_scales.shape)}")
-    if tuple(b_scales.shape) not in (_scale_shape(N, K, "row"), _scale_shape(N, K, "square")):
-        raise SageError(f"b_scales must be {_scale_shape(N, K, 'row')} or {_scale_shape(N, K, 'square')}, "
-                        f"got {tuple(b_scales.shape)}")
-    block = "square" if tuple(b_scales.shape) == _scale_shape(N, K, "square") else "row"
+    kb, squares = -(-K // 128), -(-N // 128)
+    if a_scales.shape != (kb, M):
+        raise SageError(f"a_scales must be {(kb, M)}, got {tuple(a_scales.shape)}")
+    block = 1 if b_scales.shape == (kb, squares) else 0
+    if not block and b_scales.shape != (kb, N):
+        raise SageError(f"b_scales must be {(kb, N)} (rows) or {(kb, squares)} (squares), got {tuple(b_scales.shape)}")
     if bias is not None:
         _dev(bias, torch.float32, "bias", 1)
         if bias.shape[0] != N:
@@ -676,10 +677,10 @@ def matmul_fp8(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     dtype = dtype or (torch.bfloat16 if out is None else out.dtype)
     if dtype not in _ROW_TYPES:
         raise SageError("dtype must be float32 or bfloat16")
-    out = _result(out, (M, N), dtype, a.device)
+    out = _result(out, (M, N), dtype, a)
     lib = load_library()
     ws = _scratch(workspace, lib.sage_matmul_fp8_workspace_bytes(M, N, K), a.device)
-    _check(lib.sage_matmul_fp8(_ptr(a), _ptr(a_scales), M, _ptr(b), _ptr(b_scales), BLOCKS[block], N, K, _ptr(bias),
+    _check(lib.sage_matmul_fp8(_ptr(a), _ptr(a_scales), M, _ptr(b), _ptr(b_scales), block, N, K, _ptr(bias),
                                int(bool(relu)), int(bool(fast_accum)), _ptr(out), TYPES[dtype], _ptr(ws), _size(ws), _stream()))
     return out
 
