@@ -443,23 +443,24 @@ __global__ void __launch_bounds__(256) prompt_sum_kernel(PromptItems items, cons
   for (int p = 0; p < grid.pieces; ++p) fin.template write<V, kAligned>(zero, zero, 0, q, p);
 }
 
-// Few tokens: a workgroup per prompt and piece, whose 16 lane groups take every
-// 16th token. One launch, no partial sums in memory.
-template <class T, class O, int V, bool kAligned>
-__global__ void __launch_bounds__(256) prompt_whole_kernel(PromptItems items, const int32_t* __restrict__ offsets,
-                                                           const T* __restrict__ src, int d, int pieces, Finish<O, false> fin) {
-  __shared__ float sums[16][kGroup * V];
-  __shared__ int counts[16];
+// Few tokens: a workgroup per prompt and piece, whose kGroups lane groups take every
+// kGroups-th token. One launch, no partial sums in memory.
+template <int kGroups, class T, class O, int V, bool kAligned>
+__global__ void __launch_bounds__(kGroups * kGroup) prompt_whole_kernel(PromptItems items, const int32_t* __restrict__ offsets,
+                                                                        const T* __restrict__ src, int d, int pieces,
+                                                                        Finish<O, false> fin) {
+  __shared__ float sums[kGroups][kGroup * V];
+  __shared__ int counts[kGroups];
   const int q = blockIdx.x / pieces, piece = blockIdx.x % pieces;
   const int l = threadIdx.x % kGroup, g = threadIdx.x / kGroup;
   const int b = max(offsets[q], 0), e = min(offsets[q + 1], items.T);
   float acc[V] = {};
   int count = 0;
-  for (int i0 = b + g; i0 < e; i0 += 16 * kTurn) {
+  for (int i0 = b + g; i0 < e; i0 += kGroups * kTurn) {
     Cols<T, V, kAligned> v[kTurn];
     int row[kTurn];
 #pragma unroll
-    for (int u = 0; u < kTurn; ++u) row[u] = i0 + u * 16 < e ? items.source(i0 + u * 16) : -1;
+    for (int u = 0; u < kTurn; ++u) row[u] = i0 + u * kGroups < e ? items.source(i0 + u * kGroups) : -1;
 #pragma unroll
     for (int u = 0; u < kTurn; ++u)
       if (row[u] >= 0) v[u].load(src + (long long)row[u] * d, piece, d);
@@ -475,7 +476,8 @@ __global__ void __launch_bounds__(256) prompt_whole_kernel(PromptItems items, co
   if (l == 0) counts[g] = count;
   __syncthreads();
   if (g > 0) return;
-  for (int i = 1; i < 16; ++i) {
+#pragma unroll 4
+  for (int i = 1; i < kGroups; ++i) {
     count += counts[i];
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] += sums[i][l * V + j];
@@ -513,8 +515,17 @@ __global__ void __launch_bounds__(256) token_sum_kernel(SortedItems items, const
     missing &= missing - 1;
     const long long at = (long long)v * d;
     if (kAligned) {
-      for (int c = lane * 4; c < d; c += 256)
-        stream_store(fin.add ? stream_load(fin.add + at + c) : floatx4{}, fin.out + at + c);
+      for (int c0 = lane * 4; c0 < d; c0 += 1024) {      // four pieces in flight
+        floatx4 v[4] = {};
+        if (fin.add) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (c0 + u * 256 < d) v[u] = stream_load(fin.add + at + c0 + u * 256);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c0 + u * 256 < d) stream_store(v[u], fin.out + at + c0 + u * 256);
+      }
     } else {
       for (int c = lane; c < d; c += 64) fin.out[at + c] = fin.add ? fin.add[at + c] : 0.0f;
     }
@@ -677,6 +688,76 @@ __global__ void __launch_bounds__(kSortThreads) token_scatter_kernel(
   }
 }
 
+// The same order of up to kRankTokens tokens in one launch: a token's place is the
+// number of keys below its own, and of equal ones before it. A workgroup places 16
+// tokens, 16 threads each, against all keys in LDS; it finds their prompts, and
+// the first valid token of a prompt writes the number of its valid tokens (from a
+// prefix count).
+constexpr int kRankTokens = 8192;
+__global__ void __launch_bounds__(256) token_rank_kernel(PromptItems items, const int32_t* __restrict__ offsets, int Q,
+                                                         uint32_t* __restrict__ keys_out, uint32_t* __restrict__ rows_out,
+                                                         int32_t* __restrict__ valid) {
+  __shared__ __attribute__((aligned(16))) uint32_t keys[kRankTokens];
+  __shared__ uint16_t before[kRankTokens + 1];           // valid tokens before each (of those in prompts)
+  __shared__ int wave_sum[4];
+  const int T = items.T, V = items.V, lane = (int)lane_id(), w = threadIdx.x / 64;
+  const int begin = offsets ? max(offsets[0], 0) : 0, end = offsets ? min(offsets[Q], T) : T;
+  const int padded = (T + 63) & ~63;
+  for (int i = threadIdx.x; i < padded; i += 256) {
+    const int id = i < T && i >= begin && i < end ? items.tokens[i] : -1;
+    keys[i] = i >= T ? 0xFFFFFFFFu : (unsigned)id < (unsigned)V ? (uint32_t)id : (uint32_t)V;
+  }
+  __syncthreads();
+  if (valid) {
+    const int per = padded / 256 + (padded % 256 != 0), i0 = threadIdx.x * per;
+    int mine = 0;
+    for (int i = i0; i < min(i0 + per, T); ++i) mine += keys[i] < (uint32_t)V;
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += y;
+    }
+    if (lane == 63) wave_sum[w] = incl;
+    __syncthreads();
+    int run = incl - mine;
+    for (int k = 0; k < w; ++k) run += wave_sum[k];
+    for (int i = i0; i < min(i0 + per, T); ++i) {
+      before[i] = (uint16_t)run;
+      run += keys[i] < (uint32_t)V;
+    }
+    if (i0 < T && i0 + per >= T) before[T] = (uint16_t)run;
+    __syncthreads();
+  }
+  const int i = blockIdx.x * 16 + threadIdx.x / 16, part = threadIdx.x % 16;
+  const uint32_t key = keys[min(i, T - 1)];
+  const int own = blockIdx.x * 16 / 64 * 64;             // the 64 keys that hold the workgroup's tokens
+  int place = 0;
+  for (int j = 0; j < padded; j += 64) {
+    const uint4 k = *reinterpret_cast<const uint4*>(keys + j + part * 4);
+    if (j < own) {
+      place += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+    } else if (j > own) {
+      place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+    } else {
+      const int at = j + part * 4;
+      place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+      place += (k.x == key && at < i) + (k.y == key && at + 1 < i) + (k.z == key && at + 2 < i) + (k.w == key && at + 3 < i);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) place += __shfl_xor(place, o, 16);
+  if (part > 0 || i >= T) return;
+  const bool in = offsets && i >= begin && i < end;
+  const int q = in ? last_at_most(offsets, 0, Q, i) : -1;
+  keys_out[place] = key;
+  rows_out[place] = offsets ? (uint32_t)max(q, 0) : (uint32_t)i;
+  if (valid && q >= 0 && key < (uint32_t)V) {
+    const int b = max(offsets[q], 0), e = min(offsets[q + 1], T);
+    if (before[i] == before[b]) valid[q] = (int)before[e] - (int)before[b];
+  }
+}
+
 __global__ void __launch_bounds__(256) clear_kernel(int32_t* __restrict__ p, int n) {
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i < n) p[i] = 0;
@@ -731,9 +812,12 @@ hipError_t find_prompts(const int32_t* offsets, int T, int Q, int32_t* prompt, h
   return hipGetLastError();
 }
 
-// Few tokens of few prompts: a workgroup per prompt adds them (a prompt that has
-// them all is 32 turns of it).
+// Few tokens of few prompts: a workgroup per prompt and piece adds them, of 64 lane
+// groups where a prompt may be long (1,727 tokens of one prompt: 36 us a call with
+// 16 groups, 12 with 64; 2,960 tokens of 348 prompts: 9 us, the chunks' three
+// launches 22). A prompt that has them all is 8 turns.
 constexpr int kWholeTokens = 4096, kWholeGroups = 4096;
+constexpr int kShortTokens = 2048, kShortPrompt = 128;   // 16 groups: at most so many tokens, and in the mean per prompt
 
 template <class T, class O, bool kAligned>
 hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, int d, float scale, Prompts p, void* out,
@@ -751,8 +835,12 @@ hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, i
   const int pieces = piece_count(d, kVec);
   if (T_ <= kWholeTokens && (long long)p.Q * pieces <= kWholeGroups) {
     LaunchScope scope("prompt_whole_kernel", stream);
-    prompt_whole_kernel<T, O, kVec, kAligned><<<(unsigned)p.Q * pieces, 256, 0, stream>>>(
-        PromptItems{tokens, nullptr, T_, V}, p.offsets, src, d, pieces, fin);
+    const PromptItems items{tokens, nullptr, T_, V};
+    const unsigned grid = (unsigned)p.Q * pieces;
+    if (T_ > kShortTokens || T_ / p.Q >= kShortPrompt)
+      prompt_whole_kernel<64, T, O, kVec, kAligned><<<grid, 1024, 0, stream>>>(items, p.offsets, src, d, pieces, fin);
+    else
+      prompt_whole_kernel<16, T, O, kVec, kAligned><<<grid, 256, 0, stream>>>(items, p.offsets, src, d, pieces, fin);
     return hipGetLastError();
   }
   const PartialLayout l = partial_layout(T_, d, kVec);
@@ -827,15 +915,21 @@ hipError_t embed_grad_with(const int32_t* tokens, int T_, const void* grad, int 
   int32_t* prompt = p.offsets ? reinterpret_cast<int32_t*>(base + l.prompt) : nullptr;
   const PromptItems prompts{tokens, prompt, T_, V};
   hipError_t e;
-  if (prompt && T_ > 0 && (e = find_prompts(p.offsets, T_, p.Q, prompt, stream)) != hipSuccess) return e;
-  if (valid && T_ > 0) {
+  int at = 0;                                            // where the sorted list is
+  if (T_ > 0 && T_ <= kRankTokens) {
+    LaunchScope scope("token_rank_kernel", stream);
+    token_rank_kernel<<<ceil_div(T_, 16), 256, 0, stream>>>(prompts, p.offsets, p.Q, keys[0], rows[0], valid);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const bool sort = T_ > kRankTokens;
+  if (prompt && sort && (e = find_prompts(p.offsets, T_, p.Q, prompt, stream)) != hipSuccess) return e;
+  if (valid && sort) {
     LaunchScope scope("clear_kernel", stream);
     clear_kernel<<<ceil_div(p.Q, 256), 256, 0, stream>>>(valid, p.Q);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  int at = 0;                                            // where the sorted list is
   const int bits = key_bits(V);
-  for (int shift = 0; T_ > 0 && shift < bits; shift += kSortBits) {
+  for (int shift = 0; sort && shift < bits; shift += kSortBits) {
     const bool first = shift == 0;
     {
       LaunchScope scope("token_count_kernel", stream);

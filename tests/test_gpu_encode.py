@@ -54,7 +54,9 @@ def test_embed_tokens(T, V, d, ttype, otype):
     (1, 1, 3, 8, BF16, BF16, True), (64, 1, 40, 512, BF16, F32, False), (65, 1, 40, 520, BF16, F32, True),
     (211, 1, 320, 768, BF16, BF16, True), (5000, 1, 300, 96, F32, F32, False), (3, 9, 5, 40, F32, F32, True),
     (700, 700, 90, 33, BF16, F32, False), (4096, 64, 1000, 128, BF16, F32, True), (9000, 37, 800, 1001, F32, F32, True),
-    (20000, 3000, 4000, 256, BF16, BF16, False), (70001, 5, 2000, 64, BF16, F32, True), (300, 20, 50, 4100, F32, BF16, False)])
+    (20000, 3000, 4000, 256, BF16, BF16, False), (70001, 5, 2000, 64, BF16, F32, True), (300, 20, 50, 4100, F32, BF16, False),
+    (2048, 1, 300, 200, F32, F32, True), (2049, 1, 300, 200, F32, F32, True), (2048, 15, 300, 136, BF16, F32, False),
+    (1500, 1400, 300, 1024, BF16, BF16, True)])
 def test_embed_prompts(T, Q, V, d, ttype, otype, mean):
     tok, off = tokens_like(T, V, T + Q, pad=0.1), cut(T, Q, T + d)
     table = torch.randn(V, d, generator=gen(d)).to(ttype).cuda()
@@ -104,7 +106,8 @@ def test_embed_nan_row_stays_in_its_prompt():
 GRADS = [(1, 0, 1, 1, F32, False), (5, 0, 3, 40, BF16, False), (1024, 0, 511, 64, BF16, False), (1025, 0, 512, 64, F32, False),
          (6500, 0, 5003, 77, BF16, False), (30000, 0, 20, 136, F32, False), (4097, 0, 262145, 8, BF16, False),
          (211, 1, 3200, 768, BF16, True), (3, 9, 5, 40, F32, True), (20000, 300, 3000, 100, F32, True),
-         (50000, 7, 900, 520, BF16, False), (9000, 900, 40, 64, BF16, True)]
+         (50000, 7, 900, 520, BF16, False), (9000, 900, 40, 64, BF16, True), (8192, 33, 700, 72, F32, True),
+         (8193, 33, 700, 72, F32, True), (8192, 0, 70000, 24, BF16, False), (64, 64, 9, 16, BF16, True), (2000, 1, 2, 96, F32, True)]
 
 
 @pytest.mark.parametrize("T,Q,V,d,gtype,mean", GRADS)
