@@ -1,0 +1,163 @@
+"""From token ids to scheduling decisions: a prompt encoder on the library's
+operators, in front of a history store.
+
+The predictor compares prompts by embeddings (Sec. 3.1), which the paper takes
+from an embedding model that it does not name. This one is a deep averaging
+network: a prompt's first vector is the scaled mean of its tokens' embeddings,
+and each layer adds a two-layer perceptron of the normalised vector,
+
+    x_0     = scale * mean over the prompt's tokens of table[token]
+    x_{l+1} = x_l + W2_l relu(W1_l norm(x_l) + b1_l) + b2_l
+    output  = x_L / |x_L|
+
+with the norms' outputs, the hidden vectors and the weights in 8 bits (scales
+per block of 128) and everything between in bf16. Weights are kept in fp32, and
+`refresh` lays them out again after they change. `gradients` runs the backward
+pass, its products in 8 bits as well (a rounding counts as the identity, and a
+hidden value is on the side of the ReLU where the forward pass had it).
+
+    python -m paper_2603_07917_amd.encoder          # a small run on the GPU
+"""
+from __future__ import annotations
+
+import math
+from dataclasses import dataclass, field
+from typing import List, Optional
+
+import torch
+
+from . import sage
+
+FP8 = torch.float8_e4m3fn
+FINAL_EPS = 1e-12
+
+
+@dataclass
+class Layer:
+    gain: torch.Tensor                                   # [d]
+    w1: torch.Tensor                                     # [hidden, d]
+    b1: torch.Tensor
+    w2: torch.Tensor                                     # [d, hidden]
+    b2: torch.Tensor
+    laid: dict = field(default_factory=dict)             # 8-bit forms of the weights
+
+    def form(self, name: str, transpose: bool):
+        key = (name, transpose)
+        if key not in self.laid:
+            self.laid[key] = sage.quantize(getattr(self, name), block="square", transpose=transpose)
+        return self.laid[key]
+
+
+class PromptEncoder:
+    """Embeddings of ragged prompts: tokens [T] int32 and offsets [Q + 1] int32
+    (prompt q is tokens[offsets[q]:offsets[q + 1]]) to unit vectors [Q, d]."""
+
+    def __init__(self, vocab: int, d: int, hidden: int, layers: int, seed: int = 0, eps: float = 1e-6,
+                 device: str = "cuda"):
+        if d % 32 != 0:
+            raise sage.SageError("d must be a multiple of 32, as the store's rows are")
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+        rand = lambda *shape: torch.randn(*shape, generator=g, device=device)
+        self.vocab, self.d, self.eps, self.scale = vocab, d, eps, 1.0
+        self.table = rand(vocab, d)
+        self.layers: List[Layer] = [
+            Layer(torch.ones(d, device=device), rand(hidden, d) / math.sqrt(d), torch.zeros(hidden, device=device),
+                  rand(d, hidden) / math.sqrt(hidden), torch.zeros(d, device=device)) for _ in range(layers)]
+        self.unit = torch.full((d,), 1.0 / math.sqrt(d), device=device)
+        self.refresh()
+
+    def refresh(self):
+        """Lays the weights out again; call it after they change."""
+        self.rows = sage.ingest_bf16(self.table)
+        for layer in self.layers:
+            layer.laid.clear()
+
+    def encode(self, tokens: torch.Tensor, offsets: torch.Tensor, saved: Optional[list] = None) -> torch.Tensor:
+        """Unit-norm fp32 embeddings [Q, d]; `saved` collects what `gradients` needs."""
+        x = sage.embed(tokens, self.rows, scale=self.scale, offsets=offsets, mean=True)
+        branch = None
+        for layer in self.layers:
+            q, scales, total = sage.rms_norm(x if branch is None else branch, layer.gain,
+                                             residual=None if branch is None else x, eps=self.eps, dtype=FP8)
+            x = x if total is None else total
+            h = sage.matmul_fp8(q, scales, *layer.form("w1", False), bias=layer.b1, relu=True, fast_accum=True)
+            branch = sage.matmul_fp8(*sage.quantize(h), *layer.form("w2", False), bias=layer.b2, fast_accum=True)
+            if saved is not None:
+                saved.append((x, h))
+        out, _, total = sage.rms_norm(x if branch is None else branch, self.unit, residual=None if branch is None else x,
+                                      eps=FINAL_EPS, dtype=torch.float32)
+        if saved is not None:
+            saved.append(x if total is None else total)
+        return out
+
+    def decide(self, store: sage.Store, tokens: torch.Tensor, offsets: torch.Tensor):
+        """One scheduling decision for a batch of prompts: encode, then Store.decide
+        (predict, cost and index, rank) with their lengths."""
+        return store.decide(self.encode(tokens, offsets), (offsets[1:] - offsets[:-1]).contiguous())
+
+    def gradients(self, tokens: torch.Tensor, offsets: torch.Tensor, saved: list, grad: torch.Tensor,
+                  add: Optional[torch.Tensor] = None) -> dict:
+        """Gradients of the weights from `grad` [Q, d], that of the embeddings of
+        the `encode` call that filled `saved`: {"table": [vocab, d], "layers":
+        [{"gain", "w1", "b1", "w2", "b2"}, ...]}, all fp32. `add` [vocab, d] is
+        a gradient of the table to add to, in place."""
+        dx, _ = sage.rms_norm_grad(grad.to(torch.bfloat16), saved[-1], self.unit, eps=FINAL_EPS)
+        found = []
+        for layer, (x, h) in zip(reversed(self.layers), reversed(saved[:-1])):
+            dy8 = sage.quantize(dx)
+            dh = sage.matmul_fp8(*dy8, *layer.form("w2", True), fast_accum=True)
+            dh = torch.where(h > 0, dh, torch.zeros_like(dh))
+            dw2 = sage.matmul_fp8(*sage.quantize(dx, transpose=True), *sage.quantize(h, transpose=True), dtype=torch.float32)
+            n, _, _ = sage.rms_norm(x, layer.gain, eps=self.eps)
+            dw1 = sage.matmul_fp8(*sage.quantize(dh, transpose=True), *sage.quantize(n, transpose=True), dtype=torch.float32)
+            dn = sage.matmul_fp8(*sage.quantize(dh), *layer.form("w1", True), fast_accum=True)
+            b1, b2 = dh.sum(0, dtype=torch.float32), dx.sum(0, dtype=torch.float32)
+            dx, dgain = sage.rms_norm_grad(dn, x, layer.gain, eps=self.eps, grad_total=dx)
+            found.append({"gain": dgain, "w1": dw1, "b1": b1, "w2": dw2, "b2": b2})
+        table = sage.embed_grad(tokens, dx, self.vocab, scale=self.scale, offsets=offsets, mean=True, add=add, out=add)
+        return {"table": table, "layers": found[::-1]}
+
+    def step(self, grads: dict, rate: float):
+        """One step of gradient descent, and the new layouts."""
+        self.table -= rate * grads["table"]
+        for layer, g in zip(self.layers, grads["layers"]):
+            for name, value in g.items():
+                getattr(layer, name).sub_(value, alpha=rate)
+        self.refresh()
+
+
+def main():
+    """Encodes a batch of random prompts, decides their order against a store of
+    other prompts' embeddings, and pulls each prompt towards a target of its own
+    for a few steps."""
+    from . import workloads
+    torch.manual_seed(0)
+    vocab, d, Q, T = 5000, 384, 256, 20000
+    enc = PromptEncoder(vocab, d, 1024, 2)
+
+    def prompts(n, total):
+        tokens = torch.randint(0, vocab, (total,), device="cuda", dtype=torch.int32)
+        cuts, _ = torch.sort(torch.randint(0, total + 1, (n - 1,), device="cuda", dtype=torch.int32))
+        ends = torch.tensor([0, total], device="cuda", dtype=torch.int32)
+        return tokens, torch.cat([ends[:1], cuts, ends[1:]])
+
+    past = enc.encode(*prompts(4096, 300000))
+    edges, reprs = (torch.from_numpy(a).cuda() for a in workloads.log_bins(8192, 128))
+    lens = torch.randint(1, 8192, (4096,), device="cuda", dtype=torch.int32)
+    store = sage.Store(past, lens, edges, reprs, k=32, tau=0.1)
+    tokens, offsets = prompts(Q, T)
+    ids, sims, *_, order = enc.decide(store, tokens, offsets)
+    print(f"decided {Q} prompts of {T} tokens: nearest similarity {sims[:, 0].mean().item():.3f}, "
+          f"first served {order[:4].tolist()}")
+    target = torch.nn.functional.normalize(torch.randn(Q, d, device="cuda"), dim=1)
+    for k in range(5):
+        saved = []
+        e = enc.encode(tokens, offsets, saved)
+        loss = (1.0 - (e * target).sum(1)).mean()
+        enc.step(enc.gradients(tokens, offsets, saved, -target / Q), 0.3)
+        print(f"step {k}: mean distance from the targets {loss.item():.4f}")
+
+
+if __name__ == "__main__":
+    main()
