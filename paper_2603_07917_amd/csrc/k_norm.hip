@@ -282,9 +282,9 @@ hipError_t norm_grad_by_width(const void* grad, const void* total, int M, int d,
 template <class T, bool kAligned>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict__ x, int M, int K, int kb,
                                                             uint8_t* __restrict__ q, float* __restrict__ scales) {
-  const long long blk = ((long long)blockIdx.x * 256 + threadIdx.x) / 16;
-  if (blk >= (long long)M * kb) return;
-  const int row = (int)(blk / kb), b = (int)(blk % kb), in_block = threadIdx.x % 16;
+  const unsigned blk = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^28
+  const int row = (int)(blk / (unsigned)kb), b = (int)(blk % (unsigned)kb), in_block = threadIdx.x % 16;
+  if (row >= M) return;
   const int col = b * kBlock + in_block * kCols, kp = (K + 15) & ~15;
   float v[kCols];
   load_row<T, kCols, kAligned>(v, x + (long long)row * K, col, K);
@@ -392,8 +392,7 @@ hipError_t quantize_by_block(const void* xv, int M, int K, bool square, bool tra
   if (!square && !transpose) {
     LaunchScope scope("quantize_rows_kernel", stream);
     const int kb = ceil_div(K, kBlock);
-    const long long threads = (long long)M * kb * 16;
-    quantize_rows_kernel<T, kAligned><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(x, M, K, kb, q, scales);
+    quantize_rows_kernel<T, kAligned><<<(unsigned)(((long long)M * kb + 15) / 16), 256, 0, stream>>>(x, M, K, kb, q, scales);
     return hipGetLastError();
   }
   LaunchScope scope("quantize_tile_kernel", stream);

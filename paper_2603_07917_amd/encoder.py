@@ -133,7 +133,7 @@ def main():
     for a few steps."""
     from . import workloads
     torch.manual_seed(0)
-    vocab, d, Q, T = 5000, 384, 256, 20000
+    vocab, d, Q, T = 5000, 384, 256, 2000
     enc = PromptEncoder(vocab, d, 1024, 2)
 
     def prompts(n, total):
@@ -155,7 +155,7 @@ def main():
         saved = []
         e = enc.encode(tokens, offsets, saved)
         loss = (1.0 - (e * target).sum(1)).mean()
-        enc.step(enc.gradients(tokens, offsets, saved, -target / Q), 0.3)
+        enc.step(enc.gradients(tokens, offsets, saved, -target / Q), 4.0)
         print(f"step {k}: mean distance from the targets {loss.item():.4f}")
 
 

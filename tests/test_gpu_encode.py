@@ -393,6 +393,48 @@ def test_matmul_gradients_of_a_layer():
         assert float((got.double() - exact).norm() / exact.norm()) < 2 * 2.0 ** -4
 
 
+# ---------------------------------------------------- offsets beyond 32 bits
+def test_rows_beyond_4_gib_of_a_table():
+    V, d = 2_200_000, 1024                               # 4.5 GB in bf16, 9 GB of gradient
+    table = torch.zeros(V, d, dtype=BF16, device="cuda")
+    last = torch.tensor([0, V - 1, V - 2, 1_100_000, 2_097_152], dtype=torch.int32, device="cuda")
+    rows = torch.randn(5, d, generator=gen(1)).to(BF16).cuda()
+    table[last.long()] = rows
+    assert torch.equal(sage.embed(last, table), rows)
+    off = torch.tensor([0, 2, 5], dtype=torch.int32, device="cuda")
+    want, mag, n = ref.embed(torch.arange(5, dtype=torch.int32), rows, 1.0, off, True)
+    close(sage.embed(last, table, offsets=off, mean=True, dtype=F32), want, mag * (n + 4) * U32)
+    del table
+    grad = sage.embed_grad(last, rows, V)
+    assert torch.equal(grad[last.long()], rows.float())
+    grad[last.long()] = 0
+    assert not grad.any()
+
+
+def test_matrices_beyond_4_gib():
+    M, d = 2_200_000, 1024
+    x = torch.zeros(M, d, dtype=BF16, device="cuda")
+    tail = torch.randn(3, d, generator=gen(1)).to(BF16).cuda()
+    x[-3:] = tail
+    gain = torch.ones(d, device="cuda")
+    q, scales, _ = sage.rms_norm(x, gain, dtype=FP8)
+    q3, s3, _ = sage.rms_norm(tail, gain, dtype=FP8)
+    ref.same_e4m3(q[-3:], q3)
+    assert torch.equal(scales[:, -3:], s3)
+    q, scales = sage.quantize(x)
+    q3, s3 = sage.quantize(tail)
+    ref.same_e4m3(q[-3:], q3)
+    assert torch.equal(scales[:, -3:], s3)
+    del x
+    b, sb = sage.quantize(torch.randn(24, d, generator=gen(2)).cuda())
+    big = torch.zeros(4_400_000, d, dtype=FP8, device="cuda")    # 4.5 GB of rows
+    big[-3:] = q3
+    sa = torch.ones(d // 128, 4_400_000, device="cuda")
+    sa[:, -3:] = s3
+    want, mag = ref.matmul(q3, s3, b, sb, "row", None, False)
+    close(sage.matmul_fp8(big, sa, b, sb, dtype=F32)[-3:], want, mag * (d + 4) * U32)
+
+
 # ------------------------------------------------------- streams and graphs
 def test_on_another_stream_and_in_a_graph():
     T, Q, V, d, N = 3000, 40, 500, 256, 384
