@@ -30,7 +30,7 @@ constexpr int kTurn = 8;                                 // rows in flight per l
 
 // ------------------------------------------------------- lookup per token
 // Each thread copies pieces of 8 columns; a workgroup owns kRows tokens.
-template <class T, class O, bool kAligned>
+template <class T, class O, bool kWhole>
 __global__ void __launch_bounds__(256) embed_tokens_kernel(const int32_t* __restrict__ tokens, int T_, const T* __restrict__ table,
                                                            int V, int d, int rows, float scale, O* __restrict__ out) {
   const int pieces = (d + 7) / 8;
@@ -39,11 +39,11 @@ __global__ void __launch_bounds__(256) embed_tokens_kernel(const int32_t* __rest
     const int r = i / pieces, col = (i - r * pieces) * 8;
     const int id = tokens[first + r];
     float v[8];
-    load_row<T, 8, kAligned>(v, table + (long long)((unsigned)id < (unsigned)V ? id : 0) * d,
+    load_row<T, 8, kWhole>(v, table + (long long)((unsigned)id < (unsigned)V ? id : 0) * d,
                              (unsigned)id < (unsigned)V ? col : d, d);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= scale;
-    store_row<O, 8, kAligned>(v, out + (long long)(first + r) * d, col, d);
+    store_row<O, 8, kWhole>(v, out + (long long)(first + r) * d, col, d);
   }
 }
 
@@ -99,25 +99,24 @@ struct SortedItems {                                     // token positions or p
   __device__ __forceinline__ float weight(int i) const { return valid ? __fdiv_rn(1.0f, (float)valid[rows[i]]) : 1.0f; }
 };
 
-// The columns of a lane in piece p of a row: V = 16 bytes of consecutive ones,
-// or (unaligned rows) every 16th, so that neighbouring lanes read neighbouring
-// elements. Kept as loaded; to_f32 gives the values.
-template <class T, int V, bool kAligned>
+// The columns of a lane in piece p of a row: V = 16 bytes of consecutive ones, kept
+// as loaded.
+template <class T, int V, bool kWhole>
 struct Cols {
   union {
-    uint4 bits;
+    uintx4 bits;
     T t[V];
   };
   __device__ __forceinline__ void load(const T* row, int piece, int d) {
-    const int l = (int)lane_id() % kGroup;
-    if constexpr (kAligned) {
-      const int c = (piece * kGroup + l) * V;
-      bits = c < d ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
+    const int c = (piece * kGroup + (int)lane_id() % kGroup) * V;
+    if (kWhole ? c < d : c + V <= d) {
+      bits = reinterpret_cast<const Bits16*>(row + c)->v;
     } else {
+      bits = uintx4{};
+      if constexpr (!kWhole) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = (piece * V + j) * kGroup + l;
-        t[j] = c < d ? row[c] : (T)0.0f;
+        for (int j = 0; j < V; ++j)
+          if (c + j < d) t[j] = row[c + j];
       }
     }
   }
@@ -130,31 +129,13 @@ struct Cols {
     for (int j = 0; j < V; ++j) acc[j] = fmaf((float)t[j], w, acc[j]);
   }
 };
-template <int V, bool kAligned>
+template <int V, bool kWhole>
 __device__ __forceinline__ void load_cols(float (&v)[V], const float* row, int piece, int d) {
-  const int l = (int)lane_id() % kGroup;
-  if constexpr (kAligned) {
-    load_row<float, V, true>(v, row, (piece * kGroup + l) * V, d);
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (piece * V + j) * kGroup + l;
-      v[j] = c < d ? row[c] : 0.0f;
-    }
-  }
+  load_row<float, V, kWhole>(v, row, (piece * kGroup + (int)lane_id() % kGroup) * V, d);
 }
-template <class T, int V, bool kAligned>
+template <class T, int V, bool kWhole>
 __device__ __forceinline__ void store_cols(const float (&v)[V], T* row, int piece, int d) {
-  const int l = (int)lane_id() % kGroup;
-  if constexpr (kAligned) {
-    store_row<T, V, true>(v, row, (piece * kGroup + l) * V, d);
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (piece * V + j) * kGroup + l;
-      if (c < d) row[c] = (T)v[j];
-    }
-  }
+  store_row<T, V, kWhole>(v, row, (piece * kGroup + (int)lane_id() % kGroup) * V, d);
 }
 
 // Partial sums: two rows of d fp32 per chunk, [0] of the segment that was open
@@ -166,12 +147,13 @@ struct Partials {
 };
 // A gradient's table passes by once, and should not push the rows that the sums
 // gather out of the L2s (131,072 x 1,024 with add: 407 -> 389 us).
-typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+typedef float floatx4_any __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ floatx4 stream_load(const float* p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(p));
+  const floatx4_any v = __builtin_nontemporal_load(reinterpret_cast<const floatx4_any*>(p));
+  return floatx4{v.x, v.y, v.z, v.w};
 }
 __device__ __forceinline__ void stream_store(floatx4 v, float* p) {
-  __builtin_nontemporal_store(v, reinterpret_cast<floatx4*>(p));
+  __builtin_nontemporal_store(floatx4_any{v[0], v[1], v[2], v[3]}, reinterpret_cast<floatx4_any*>(p));
 }
 
 // What a finished sum becomes: (x scale, / count for a mean) + add, rounded.
@@ -183,36 +165,36 @@ struct Finish {
   float scale;
   bool mean;
   int d;
-  template <int V, bool kAligned>
+  template <int V, bool kWhole>
   __device__ __forceinline__ void load_add(float (&held)[V], int seg, int piece) const {
     const float* row = add + (long long)seg * d;
-    if constexpr (kStream && kAligned) {
-      const int c = (piece * kGroup + (int)lane_id() % kGroup) * V;
-      if (c >= d) return;
+    const int c = (piece * kGroup + (int)lane_id() % kGroup) * V;
+    if (kStream && c + V <= d) {
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
         const floatx4 q = stream_load(row + c + j);
         held[j] = q[0], held[j + 1] = q[1], held[j + 2] = q[2], held[j + 3] = q[3];
       }
     } else {
-      load_cols<V, kAligned>(held, row, piece, d);
+      load_cols<V, kWhole>(held, row, piece, d);
     }
   }
-  template <int V, bool kAligned>
+  template <int V, bool kWhole>
   __device__ __forceinline__ void write(const float (&acc)[V], const float (&held)[V], int count, int seg, int piece) const {
     const float c = mean && count > 0 ? __fdiv_rn(scale, (float)count) : scale;
     float v[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] = add ? fmaf(acc[j], c, held[j]) : acc[j] * c;
     O* row = out + (long long)seg * d;
-    if constexpr (kStream && kAligned) {
-      const int at = (piece * kGroup + (int)lane_id() % kGroup) * V;
-      if (at >= d) return;
+    const int at = (piece * kGroup + (int)lane_id() % kGroup) * V;
+    if constexpr (kStream) {
+      if (at + V <= d) {
 #pragma unroll
-      for (int j = 0; j < V; j += 4) stream_store(floatx4{v[j], v[j + 1], v[j + 2], v[j + 3]}, row + at + j);
-    } else {
-      store_cols<O, V, kAligned>(v, row, piece, d);
+        for (int j = 0; j < V; j += 4) stream_store(floatx4{v[j], v[j + 1], v[j + 2], v[j + 3]}, row + at + j);
+        return;
+      }
     }
+    store_cols<O, V, kWhole>(v, row, piece, d);
   }
 };
 
@@ -247,7 +229,7 @@ __device__ __forceinline__ void each_lane(F&& f) {       // f(integral_constant)
 // multiple of 16; lane l of a group holds item l of the 16 in work. With kAdd
 // the rows of `add` that finished segments need are loaded beside the items':
 // most tokens of a text are rare, and a load of its own for each would wait.
-template <bool kAdd, class Items, class T, class F, int V, bool kAligned>
+template <bool kAdd, class Items, class T, class F, int V, bool kWhole>
 __device__ __forceinline__ void sum_chunks(const Items& items, const T* __restrict__ src, int d, const ChunkGrid& grid,
                                            int piece, int c0, const Partials& part, const F& fin) {
   constexpr int kTurn = kAdd && V > 4 ? 4 : 8;           // rows in flight per group
@@ -264,10 +246,10 @@ __device__ __forceinline__ void sum_chunks(const Items& items, const T* __restri
     if (cur < 0) return;
     if (open || goes_on) {
       const long long slot = 2LL * c + (open ? 0 : 1);
-      store_cols<float, V, kAligned>(acc, part.sum + slot * d, piece, d);
+      store_cols<float, V, kWhole>(acc, part.sum + slot * d, piece, d);
       if (piece == 0 && l == 0) part.count[slot] = count;
     } else {
-      fin.template write<V, kAligned>(acc, held, count, cur, piece);
+      fin.template write<V, kWhole>(acc, held, count, cur, piece);
     }
   };
   float held[V] = {};                                    // add's row of the running segment, where its last item is behind
@@ -288,14 +270,14 @@ __device__ __forceinline__ void sum_chunks(const Items& items, const T* __restri
     const bool steady = all_valid && __all(seg == cur);
     auto turn = [&](auto at) {
       constexpr int j0 = decltype(at)::value;
-      Cols<T, V, kAligned> v[kTurn];
+      Cols<T, V, kWhole> v[kTurn];
       float more[kAdd ? kTurn : 1][V];
       each_lane<kTurn>([&](auto u) {
         constexpr int k = decltype(u)::value, j = j0 + k;
         v[k].load(src + (long long)max(of_lane<j>(row), 0) * d, piece, d);
         if constexpr (kAdd) {
           const int s = of_lane<j>(add_of);
-          if (s >= 0) fin.template load_add<V, kAligned>(more[k], s, piece);
+          if (s >= 0) fin.template load_add<V, kWhole>(more[k], s, piece);
         }
       });
       each_lane<kTurn>([&](auto u) {
@@ -335,7 +317,7 @@ __device__ __forceinline__ void sum_chunks(const Items& items, const T* __restri
 // piece) add its partial sums in order. One of more than 16 further chunks is
 // left to the whole workgroup, whose 16 groups take every 16th chunk, four at a
 // time.
-template <class F, int V, bool kAligned>
+template <class F, int V, bool kWhole>
 __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid, Partials part, F fin) {
   __shared__ float sums[16][kGroup * V];
   __shared__ int counts[16];
@@ -352,17 +334,17 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
     if (seg >= 0 && run != 0xFFFFu) {
       const int n = __builtin_ctz(~run);                 // 1 to 15 further chunks
       float acc[V];
-      load_cols<V, kAligned>(acc, part.sum + (2LL * c + 1) * d, piece, d);
+      load_cols<V, kWhole>(acc, part.sum + (2LL * c + 1) * d, piece, d);
       int count = part.count[2LL * c + 1];
       float held[V] = {};
-      if (fin.add) fin.template load_add<V, kAligned>(held, seg, piece);
+      if (fin.add) fin.template load_add<V, kWhole>(held, seg, piece);
       for (int k0 = 0; k0 < n; k0 += 4) {
         float v[4][V];
         int m[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int k = c + 1 + min(k0 + u, n - 1);
-          load_cols<V, kAligned>(v[u], part.sum + 2LL * k * d, piece, d);
+          load_cols<V, kWhole>(v[u], part.sum + 2LL * k * d, piece, d);
           m[u] = part.count[2LL * k];
         }
 #pragma unroll
@@ -373,7 +355,7 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
           for (int j = 0; j < V; ++j) acc[j] += v[u][j];
         }
       }
-      fin.template write<V, kAligned>(acc, held, count, seg, piece);
+      fin.template write<V, kWhole>(acc, held, count, seg, piece);
     }
   }
   __syncthreads();
@@ -383,7 +365,7 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
     float acc[V] = {};
     int count = 0;
     if (g == 0) {
-      load_cols<V, kAligned>(acc, part.sum + (2LL * c + 1) * d, piece, d);
+      load_cols<V, kWhole>(acc, part.sum + (2LL * c + 1) * d, piece, d);
       count = part.count[2LL * c + 1];
     }
     bool more = true;
@@ -396,7 +378,7 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
         const int k = k0 + u * 16 + g;
         in = k < grid.chunks && part.head[k] == seg;
         if (in) {
-          load_cols<V, kAligned>(v[u], part.sum + 2LL * k * d, piece, d);
+          load_cols<V, kWhole>(v[u], part.sum + 2LL * k * d, piece, d);
           n[u] = part.count[2LL * k];
         }
       }
@@ -419,8 +401,8 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
         for (int j = 0; j < V; ++j) acc[j] += sums[i][l * V + j];
       }
       float held[V] = {};
-      if (fin.add) fin.template load_add<V, kAligned>(held, seg, piece);
-      fin.template write<V, kAligned>(acc, held, count, seg, piece);
+      if (fin.add) fin.template load_add<V, kWhole>(held, seg, piece);
+      fin.template write<V, kWhole>(acc, held, count, seg, piece);
     }
     __syncthreads();
   }
@@ -428,24 +410,24 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
 
 // Prompts: the chunks' sums, and (workgroups behind them) zeros for the prompts
 // that have no tokens, 16 a workgroup.
-template <class T, class O, int V, bool kAligned>
+template <class T, class O, int V, bool kWhole>
 __global__ void __launch_bounds__(256) prompt_sum_kernel(PromptItems items, const int32_t* __restrict__ offsets, int Q,
                                                          const T* __restrict__ src, int d, ChunkGrid grid,
                                                          unsigned sum_groups, Partials part, Finish<O, false> fin) {
   if (blockIdx.x < sum_groups) {
     const int2 at = grid.at(blockIdx.x, sum_groups);
-    if (at.x >= 0) sum_chunks<false, PromptItems, T, Finish<O, false>, V, kAligned>(items, src, d, grid, at.x, at.y, part, fin);
+    if (at.x >= 0) sum_chunks<false, PromptItems, T, Finish<O, false>, V, kWhole>(items, src, d, grid, at.x, at.y, part, fin);
     return;
   }
   const int q = (int)(blockIdx.x - sum_groups) * 16 + (int)threadIdx.x / kGroup;
   if (q >= Q || max(offsets[q], 0) < min(offsets[q + 1], items.T)) return;
   const float zero[V] = {};
-  for (int p = 0; p < grid.pieces; ++p) fin.template write<V, kAligned>(zero, zero, 0, q, p);
+  for (int p = 0; p < grid.pieces; ++p) fin.template write<V, kWhole>(zero, zero, 0, q, p);
 }
 
 // Few tokens: a workgroup per prompt and piece, whose kGroups lane groups take every
 // kGroups-th token. One launch, no partial sums in memory.
-template <int kGroups, class T, class O, int V, bool kAligned>
+template <int kGroups, class T, class O, int V, bool kWhole>
 __global__ void __launch_bounds__(kGroups * kGroup) prompt_whole_kernel(PromptItems items, const int32_t* __restrict__ offsets,
                                                                         const T* __restrict__ src, int d, int pieces,
                                                                         Finish<O, false> fin) {
@@ -457,7 +439,7 @@ __global__ void __launch_bounds__(kGroups * kGroup) prompt_whole_kernel(PromptIt
   float acc[V] = {};
   int count = 0;
   for (int i0 = b + g; i0 < e; i0 += kGroups * kTurn) {
-    Cols<T, V, kAligned> v[kTurn];
+    Cols<T, V, kWhole> v[kTurn];
     int row[kTurn];
 #pragma unroll
     for (int u = 0; u < kTurn; ++u) row[u] = i0 + u * kGroups < e ? items.source(i0 + u * kGroups) : -1;
@@ -483,18 +465,18 @@ __global__ void __launch_bounds__(kGroups * kGroup) prompt_whole_kernel(PromptIt
     for (int j = 0; j < V; ++j) acc[j] += sums[i][l * V + j];
   }
   const float held[V] = {};
-  fin.template write<V, kAligned>(acc, held, count, q, piece);
+  fin.template write<V, kWhole>(acc, held, count, q, piece);
 }
 
 // Tokens: the chunks' sums, and (workgroups behind them) the rows of tokens
 // that the list does not have, zeros or `add`: 128 rows a workgroup, 32 a wave,
 // whose lane i finds the first item of its token i by a binary search.
-template <bool kAdd, class T, int V, bool kAligned>
+template <bool kAdd, class T, int V, bool kWhole>
 __global__ void __launch_bounds__(256) token_sum_kernel(SortedItems items, const T* __restrict__ src, int d, ChunkGrid grid,
                                                         unsigned sum_groups, Partials part, Finish<float, true> fin) {
   if (blockIdx.x < sum_groups) {
     const int2 at = grid.at(blockIdx.x, sum_groups);
-    if (at.x >= 0) sum_chunks<kAdd, SortedItems, T, Finish<float, true>, V, kAligned>(items, src, d, grid, at.x, at.y, part, fin);
+    if (at.x >= 0) sum_chunks<kAdd, SortedItems, T, Finish<float, true>, V, kWhole>(items, src, d, grid, at.x, at.y, part, fin);
     return;
   }
   constexpr int kTake = 32;
@@ -514,21 +496,18 @@ __global__ void __launch_bounds__(256) token_sum_kernel(SortedItems items, const
     const int v = v0 + __builtin_ctzll(missing);
     missing &= missing - 1;
     const long long at = (long long)v * d;
-    if (kAligned) {
-      for (int c0 = lane * 4; c0 < d; c0 += 1024) {      // four pieces in flight
-        floatx4 v[4] = {};
-        if (fin.add) {
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            if (c0 + u * 256 < d) v[u] = stream_load(fin.add + at + c0 + u * 256);
-        }
+    for (int c0 = lane * 4; c0 < d; c0 += 1024) {        // four pieces in flight
+      floatx4 v[4] = {};
+      if (fin.add) {
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (c0 + u * 256 < d) stream_store(v[u], fin.out + at + c0 + u * 256);
+          if (c0 + u * 256 + 4 <= d) v[u] = stream_load(fin.add + at + c0 + u * 256);
       }
-    } else {
-      for (int c = lane; c < d; c += 64) fin.out[at + c] = fin.add ? fin.add[at + c] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (c0 + u * 256 + 4 <= d) stream_store(v[u], fin.out + at + c0 + u * 256);
     }
+    if (const int c = (d & ~3) + lane; c < d) fin.out[at + c] = fin.add ? fin.add[at + c] : 0.0f;
   }
 }
 
@@ -798,12 +777,12 @@ Partials partials_at(void* ws, const PartialLayout& l) {
                   reinterpret_cast<int32_t*>(p + l.head), reinterpret_cast<int32_t*>(p + l.tail)};
 }
 
-template <class F, int V, bool kAligned>
+template <class F, int V, bool kWhole>
 hipError_t join_segments(int d, const PartialLayout& l, const Partials& part, const F& fin,
                          hipStream_t stream) {
   if (l.grid.chunks <= 1) return hipSuccess;
   LaunchScope scope("segment_join_kernel", stream);
-  segment_join_kernel<F, V, kAligned><<<(unsigned)l.grid.rows() * l.grid.pieces, 256, 0, stream>>>(d, l.grid, part, fin);
+  segment_join_kernel<F, V, kWhole><<<(unsigned)l.grid.rows() * l.grid.pieces, 256, 0, stream>>>(d, l.grid, part, fin);
   return hipGetLastError();
 }
 
@@ -820,7 +799,7 @@ hipError_t find_prompts(const int32_t* offsets, int T, int Q, int32_t* prompt, h
 constexpr int kWholeTokens = 4096, kWholeGroups = 4096;
 constexpr int kShortTokens = 2048, kShortPrompt = 128;   // 16 groups: at most so many tokens, and in the mean per prompt
 
-template <class T, class O, bool kAligned>
+template <class T, class O, bool kWhole>
 hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, int d, float scale, Prompts p, void* out,
                       void* ws, hipStream_t stream) {
   constexpr int kVec = 16 / sizeof(T);
@@ -829,7 +808,7 @@ hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, i
   if (!p.offsets) {
     LaunchScope scope("embed_tokens_kernel", stream);
     const int rows = max(1, 2048 / ceil_div(d, 8));      // about eight pieces a thread
-    embed_tokens_kernel<T, O, kAligned><<<ceil_div(T_, rows), 256, 0, stream>>>(tokens, T_, src, V, d, rows, scale, dst);
+    embed_tokens_kernel<T, O, kWhole><<<ceil_div(T_, rows), 256, 0, stream>>>(tokens, T_, src, V, d, rows, scale, dst);
     return hipGetLastError();
   }
   const Finish<O, false> fin{dst, nullptr, scale, p.mean, d};
@@ -839,9 +818,9 @@ hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, i
     const PromptItems items{tokens, nullptr, T_, V};
     const unsigned grid = (unsigned)p.Q * pieces;
     if (T_ > kShortTokens || T_ / p.Q >= kShortPrompt)
-      prompt_whole_kernel<64, T, O, kVec, kAligned><<<grid, 1024, 0, stream>>>(items, p.offsets, src, d, pieces, fin);
+      prompt_whole_kernel<64, T, O, kVec, kWhole><<<grid, 1024, 0, stream>>>(items, p.offsets, src, d, pieces, fin);
     else
-      prompt_whole_kernel<16, T, O, kVec, kAligned><<<grid, 256, 0, stream>>>(items, p.offsets, src, d, pieces, fin);
+      prompt_whole_kernel<16, T, O, kVec, kWhole><<<grid, 256, 0, stream>>>(items, p.offsets, src, d, pieces, fin);
     return hipGetLastError();
   }
   const PartialLayout l = partial_layout(T_, d, kVec);
@@ -855,15 +834,15 @@ hipError_t embed_with(const int32_t* tokens, int T_, const void* table, int V, i
   {
     LaunchScope scope("prompt_sum_kernel", stream);
     const unsigned groups = (unsigned)l.grid.groups();
-    prompt_sum_kernel<T, O, kVec, kAligned><<<groups + ceil_div(p.Q, 16), 256, 0, stream>>>(items, p.offsets, p.Q, src, d, l.grid, groups, part, fin);
+    prompt_sum_kernel<T, O, kVec, kWhole><<<groups + ceil_div(p.Q, 16), 256, 0, stream>>>(items, p.offsets, p.Q, src, d, l.grid, groups, part, fin);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  return join_segments<Finish<O, false>, kVec, kAligned>(d, l, part, fin, stream);
+  return join_segments<Finish<O, false>, kVec, kWhole>(d, l, part, fin, stream);
 }
 
 template <class T, class O>
-hipError_t embed_by_alignment(const int32_t* tokens, int T_, const void* table, int V, int d, float scale, Prompts p,
+hipError_t embed_by_width(const int32_t* tokens, int T_, const void* table, int V, int d, float scale, Prompts p,
                               void* out, void* ws, hipStream_t stream) {
   return d % 8 == 0 ? embed_with<T, O, true>(tokens, T_, table, V, d, scale, p, out, ws, stream)
                     : embed_with<T, O, false>(tokens, T_, table, V, d, scale, p, out, ws, stream);
@@ -901,7 +880,7 @@ GradLayout grad_layout(int T, int Q, int d) {
   return l;
 }
 
-template <class T, bool kAligned>
+template <class T, bool kWhole>
 hipError_t embed_grad_with(const int32_t* tokens, int T_, const void* grad, int V, int d, float scale, Prompts p,
                            const float* add, float* out, void* ws, hipStream_t stream) {
   constexpr int kVec = 16 / sizeof(T);
@@ -963,12 +942,12 @@ hipError_t embed_grad_with(const int32_t* tokens, int T_, const void* grad, int 
   if (groups + fill > 0) {
     LaunchScope scope("token_sum_kernel", stream);
     const T* src = static_cast<const T*>(grad);
-    if (add) token_sum_kernel<true, T, kVec, kAligned><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
-    else token_sum_kernel<false, T, kVec, kAligned><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
+    if (add) token_sum_kernel<true, T, kVec, kWhole><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
+    else token_sum_kernel<false, T, kVec, kWhole><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
     if ((e = hipGetLastError()) != hipSuccess || T_ == 0) return e;
   }
   if (T_ == 0) return hipSuccess;
-  return join_segments<Finish<float, true>, kVec, kAligned>(d, pl, part, fin, stream);
+  return join_segments<Finish<float, true>, kVec, kWhole>(d, pl, part, fin, stream);
 }
 
 }  // namespace
@@ -978,10 +957,10 @@ size_t embed_workspace_bytes(int T, int Q, int d) { return T > 0 && Q > 0 ? part
 hipError_t launch_embed(const int32_t* tokens, int T, const void* table, Type table_type, int V, int d, float scale,
                         Prompts p, void* out, Type out_type, void* ws, hipStream_t stream) {
   if (table_type == kBF16)
-    return out_type == kBF16 ? embed_by_alignment<bf16, bf16>(tokens, T, table, V, d, scale, p, out, ws, stream)
-                             : embed_by_alignment<bf16, float>(tokens, T, table, V, d, scale, p, out, ws, stream);
-  return out_type == kBF16 ? embed_by_alignment<float, bf16>(tokens, T, table, V, d, scale, p, out, ws, stream)
-                           : embed_by_alignment<float, float>(tokens, T, table, V, d, scale, p, out, ws, stream);
+    return out_type == kBF16 ? embed_by_width<bf16, bf16>(tokens, T, table, V, d, scale, p, out, ws, stream)
+                             : embed_by_width<bf16, float>(tokens, T, table, V, d, scale, p, out, ws, stream);
+  return out_type == kBF16 ? embed_by_width<float, bf16>(tokens, T, table, V, d, scale, p, out, ws, stream)
+                           : embed_by_width<float, float>(tokens, T, table, V, d, scale, p, out, ws, stream);
 }
 
 size_t embed_grad_workspace_bytes(int T, int Q, int V, int d) {
@@ -991,11 +970,11 @@ size_t embed_grad_workspace_bytes(int T, int Q, int V, int d) {
 
 hipError_t launch_embed_grad(const int32_t* tokens, int T, const void* grad, Type grad_type, int V, int d, float scale,
                              Prompts p, const float* add, float* out, void* ws, hipStream_t stream) {
-  const bool aligned = d % 8 == 0;
+  const bool whole = d % 8 == 0;
   if (grad_type == kBF16)
-    return aligned ? embed_grad_with<bf16, true>(tokens, T, grad, V, d, scale, p, add, out, ws, stream)
+    return whole ? embed_grad_with<bf16, true>(tokens, T, grad, V, d, scale, p, add, out, ws, stream)
                    : embed_grad_with<bf16, false>(tokens, T, grad, V, d, scale, p, add, out, ws, stream);
-  return aligned ? embed_grad_with<float, true>(tokens, T, grad, V, d, scale, p, add, out, ws, stream)
+  return whole ? embed_grad_with<float, true>(tokens, T, grad, V, d, scale, p, add, out, ws, stream)
                  : embed_grad_with<float, false>(tokens, T, grad, V, d, scale, p, add, out, ws, stream);
 }
 

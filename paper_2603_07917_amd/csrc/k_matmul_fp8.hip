@@ -32,7 +32,6 @@ namespace {
 
 typedef __attribute__((__vector_size__(8 * sizeof(int)))) int intx8;
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int intx4;
-typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 mfma_bf16x8;
@@ -90,18 +89,18 @@ __device__ __forceinline__ floatx4 act(floatx4 y, bool relu) {
   return y;
 }
 // Bias, ReLU and the store of 4 neighbouring outputs of a row.
-template <class O, bool kVec>
+template <class O, bool kWhole>
 __device__ __forceinline__ void finish4(floatx4 y, floatx4 bias, bool relu, O* row, int n, int N) {
   y = act(y + bias, relu);
   const float v[4] = {y[0], y[1], y[2], y[3]};
-  store_row<O, 4, kVec>(v, row, n, N);
+  store_row<O, 4, kWhole>(v, row, n, N);
 }
-template <bool kVec>
+template <bool kWhole>
 __device__ __forceinline__ floatx4 bias4(const float* __restrict__ bias, int n, int N) {
   floatx4 v = {};
   if (bias) {
     float f[4];
-    load_row<float, 4, kVec>(f, bias, n, N);
+    load_row<float, 4, kWhole>(f, bias, n, N);
     v = floatx4{f[0], f[1], f[2], f[3]};
   }
   return v;
@@ -269,12 +268,12 @@ struct Feed {
 };
 
 // Outputs y of row m, columns n to n + 3.
-template <class O, bool kVec>
+template <class O, bool kWhole>
 __device__ __forceinline__ void put4(const Fp8Product& p, int splits, int split, float* part, int m, int n, floatx4 y,
                                      floatx4 bias) {
   if (m >= p.M || n >= p.N) return;
-  if (splits > 1) finish4<float, kVec>(y, floatx4{}, false, part + ((long long)split * p.M + m) * p.N, n, p.N);
-  else finish4<O, kVec>(y, bias, p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
+  if (splits > 1) finish4<float, kWhole>(y, floatx4{}, false, part + ((long long)split * p.M + m) * p.N, n, p.N);
+  else finish4<O, kWhole>(y, bias, p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
 }
 
 // ---------------------------------------------------------------------------
@@ -286,7 +285,7 @@ __device__ __forceinline__ void put4(const Fp8Product& p, int splits, int split,
 // conversions, 2 additions and, with a scale per row of b, 2 products: 24 to 32
 // cycles of the vector ALU, so the two workgroups of a CU keep both busy.
 // ---------------------------------------------------------------------------
-template <bool kSquare, class O, bool kVec>
+template <bool kSquare, class O, bool kWhole>
 __global__ void __launch_bounds__(256, 2) matmul_exact_kernel(Fp8Product p, TileList list, float* __restrict__ part) {
   constexpr int BM = 128, BN = 128, WM = 2;
   typedef Feed<BM, BN, 4, kSquare> F;
@@ -397,10 +396,10 @@ __global__ void __launch_bounds__(256, 2) matmul_exact_kernel(Fp8Product p, Tile
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int col = done.n0 + wn * 64 + j * 32 + q * 8 + half * 4;
-        const floatx4 bias = bias4<kVec>(p.bias, col, p.N);
+        const floatx4 bias = bias4<kWhole>(p.bias, col, p.N);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          put4<O, kVec>(p, list.splits, done.split, part, done.m0 + wm * 64 + i * 32 + l32, col,
+          put4<O, kWhole>(p, list.splits, done.split, part, done.m0 + wm * 64 + i * 32 + l32, col,
                         floatx4{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]}, bias);
       }
     cur.kb = cur.tile.kb1 - 1;
@@ -422,7 +421,7 @@ __global__ void __launch_bounds__(256, 2) matmul_exact_kernel(Fp8Product p, Tile
 // ---------------------------------------------------------------------------
 constexpr int kBehind = 3;
 
-template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kVec>
+template <int BM, int BN, int WM, int WN, bool kSquare, class O, bool kWhole>
 __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p, TileList list, float* __restrict__ part) {
   typedef Feed<BM, BN, WM * WN, kSquare> F;
   constexpr int MS = BM / WM / 16, NS = BN / WN / 16;
@@ -529,11 +528,11 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
       feed.end_block(n);
     }
     const TileAt done = cur.tile;
-    const bool octets = sizeof(O) == 2 && p.N % 8 == 0 && list.splits == 1;
+    const bool octets = sizeof(O) == 2 && list.splits == 1;
 #pragma unroll
     for (int j = 0; j < NS; j += 2) {
       const int n = done.n0 + (wn * NS + j) * 16 + g4 * 4;
-      const floatx4 bias0 = bias4<kVec>(p.bias, n, p.N), bias1 = bias4<kVec>(p.bias, n + 16, p.N);
+      const floatx4 bias0 = bias4<kWhole>(p.bias, n, p.N), bias1 = bias4<kWhole>(p.bias, n + 16, p.N);
 #pragma unroll
       for (int i = 0; i < MS; ++i) {
         const int m = done.m0 + (wm * MS + i) * 16 + l16;
@@ -544,11 +543,18 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
           const auto x = __builtin_amdgcn_permlane16_swap(bf16_pair(v0[0], v0[1]), bf16_pair(v1[0], v1[1]), false, false);
           const auto z = __builtin_amdgcn_permlane16_swap(bf16_pair(v0[2], v0[3]), bf16_pair(v1[2], v1[3]), false, false);
           const int n8 = done.n0 + (wn * NS + j + (g4 & 1)) * 16 + (g4 >> 1) * 8;
-          if (m < p.M && n8 < p.N)
-            *reinterpret_cast<uint4*>(static_cast<O*>(p.out) + (long long)m * p.N + n8) = make_uint4(x[0], z[0], x[1], z[1]);
+          O* const row = static_cast<O*>(p.out) + (long long)m * p.N;
+          if (m < p.M && n8 + 8 <= p.N) {
+            reinterpret_cast<Bits16*>(row + n8)->v = uintx4{x[0], z[0], x[1], z[1]};
+          } else if (m < p.M) {
+            const uint32_t pairs[4] = {x[0], z[0], x[1], z[1]};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (n8 + e < p.N) row[n8 + e] = (O)(e % 2 ? from_bits_hi(pairs[e / 2]) : from_bits_lo(pairs[e / 2]));
+          }
         } else {
-          put4<O, kVec>(p, list.splits, done.split, part, m, n, acc[j][i], bias0);
-          put4<O, kVec>(p, list.splits, done.split, part, m, n + 16, acc[j + 1][i], bias1);
+          put4<O, kWhole>(p, list.splits, done.split, part, m, n, acc[j][i], bias0);
+          put4<O, kWhole>(p, list.splits, done.split, part, m, n + 16, acc[j + 1][i], bias1);
         }
       }
     }
@@ -565,7 +571,7 @@ __global__ void __launch_bounds__(64 * WM * WN) matmul_fast_kernel(Fp8Product p,
 // ---------------------------------------------------------------------------
 constexpr int kFewRows = 64, kFewWaves = 8;
 
-template <int MT, bool kSquare, class O, bool kVec>
+template <int MT, bool kSquare, class O, bool kWhole>
 __global__ void __launch_bounds__(64 * kFewWaves) matmul_few_kernel(Fp8Product p) {
   __shared__ floatx4 sums[kFewWaves - 1][MT][64];
   const int lane = (int)lane_id(), w = threadIdx.x / 64;
@@ -626,12 +632,12 @@ __global__ void __launch_bounds__(64 * kFewWaves) matmul_few_kernel(Fp8Product p
 #pragma unroll
     for (int k = 0; k < kFewWaves - 1; ++k) y += sums[k][i][lane];
     const int m = i * 16 + l16, n = n0 + 4 * g4;
-    put4<O, kVec>(p, 1, 0, nullptr, m, n, y, bias4<kVec>(p.bias, n, p.N));
+    put4<O, kWhole>(p, 1, 0, nullptr, m, n, y, bias4<kWhole>(p.bias, n, p.N));
   }
 }
 
 // The splits' sums, in order.
-template <class O, bool kVec>
+template <class O, bool kWhole>
 __global__ void __launch_bounds__(256) matmul_join_kernel(Fp8Product p, int splits, const float* __restrict__ part) {
   const int quads = (p.N + 3) / 4;
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -640,11 +646,11 @@ __global__ void __launch_bounds__(256) matmul_join_kernel(Fp8Product p, int spli
   floatx4 y = {};
   for (int s = 0; s < splits; ++s) {
     float v[4];
-    load_row<float, 4, kVec>(v, part + ((long long)s * p.M + m) * p.N, n, p.N);
+    load_row<float, 4, kWhole>(v, part + ((long long)s * p.M + m) * p.N, n, p.N);
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] += v[j];
   }
-  finish4<O, kVec>(y, bias4<kVec>(p.bias, n, p.N), p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
+  finish4<O, kWhole>(y, bias4<kWhole>(p.bias, n, p.N), p.relu, static_cast<O*>(p.out) + (long long)m * p.N, n, p.N);
 }
 
 struct Plan {
@@ -670,14 +676,14 @@ unsigned grid_of(const TileList& list) {
   return std::min(((unsigned)list.size() + 7) / 8 * 8, list.bm == 256 ? 256u : 512u);
 }
 
-template <bool kSquare, class O, bool kVec>
+template <bool kSquare, class O, bool kWhole>
 hipError_t run_tiles(const Fp8Product& p, const Plan& pl, float* part, hipStream_t stream) {
   if (pl.tile == 0) {
     LaunchScope scope("matmul_few_kernel", stream);
     const unsigned grid = (unsigned)ceil_div(p.N, 16);
-    if (p.M <= 16) matmul_few_kernel<1, kSquare, O, kVec><<<grid, 64 * kFewWaves, 0, stream>>>(p);
-    else if (p.M <= 32) matmul_few_kernel<2, kSquare, O, kVec><<<grid, 64 * kFewWaves, 0, stream>>>(p);
-    else matmul_few_kernel<4, kSquare, O, kVec><<<grid, 64 * kFewWaves, 0, stream>>>(p);
+    if (p.M <= 16) matmul_few_kernel<1, kSquare, O, kWhole><<<grid, 64 * kFewWaves, 0, stream>>>(p);
+    else if (p.M <= 32) matmul_few_kernel<2, kSquare, O, kWhole><<<grid, 64 * kFewWaves, 0, stream>>>(p);
+    else matmul_few_kernel<4, kSquare, O, kWhole><<<grid, 64 * kFewWaves, 0, stream>>>(p);
     return hipGetLastError();
   }
   const TileList list{ceil_div(p.M, pl.tile), ceil_div(p.N, pl.tile), pl.splits, pl.blocks_per_split, ceil_div(p.K, kBlock),
@@ -685,20 +691,20 @@ hipError_t run_tiles(const Fp8Product& p, const Plan& pl, float* part, hipStream
   const unsigned grid = grid_of(list);
   {
     LaunchScope scope(p.fast ? "matmul_fast_kernel" : "matmul_exact_kernel", stream);
-    if (pl.tile == 256) matmul_fast_kernel<256, 256, 4, 2, kSquare, O, kVec><<<grid, 512, 0, stream>>>(p, list, part);
-    else if (p.fast) matmul_fast_kernel<128, 128, 2, 2, kSquare, O, kVec><<<grid, 256, 0, stream>>>(p, list, part);
-    else matmul_exact_kernel<kSquare, O, kVec><<<grid, 256, 0, stream>>>(p, list, part);
+    if (pl.tile == 256) matmul_fast_kernel<256, 256, 4, 2, kSquare, O, kWhole><<<grid, 512, 0, stream>>>(p, list, part);
+    else if (p.fast) matmul_fast_kernel<128, 128, 2, 2, kSquare, O, kWhole><<<grid, 256, 0, stream>>>(p, list, part);
+    else matmul_exact_kernel<kSquare, O, kWhole><<<grid, 256, 0, stream>>>(p, list, part);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1) return e;
   }
   LaunchScope scope("matmul_join_kernel", stream);
   const long long quads = (long long)p.M * ((p.N + 3) / 4);
-  matmul_join_kernel<O, kVec><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(p, pl.splits, part);
+  matmul_join_kernel<O, kWhole><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(p, pl.splits, part);
   return hipGetLastError();
 }
 
 template <bool kSquare, class O>
-hipError_t run_by_alignment(const Fp8Product& p, float* part, hipStream_t stream) {
+hipError_t run_by_width(const Fp8Product& p, float* part, hipStream_t stream) {
   const Plan pl = plan_matmul(p.M, p.N, p.K, p.fast);
   return p.N % 4 == 0 ? run_tiles<kSquare, O, true>(p, pl, part, stream) : run_tiles<kSquare, O, false>(p, pl, part, stream);
 }
@@ -713,8 +719,8 @@ size_t matmul_fp8_workspace_bytes(int M, int N, int K) {
 hipError_t launch_matmul_fp8(const Fp8Product& p, void* ws, hipStream_t stream) {
   float* part = static_cast<float*>(ws);
   if (p.out_type == kBF16)
-    return p.b_square ? run_by_alignment<true, bf16>(p, part, stream) : run_by_alignment<false, bf16>(p, part, stream);
-  return p.b_square ? run_by_alignment<true, float>(p, part, stream) : run_by_alignment<false, float>(p, part, stream);
+    return p.b_square ? run_by_width<true, bf16>(p, part, stream) : run_by_width<false, bf16>(p, part, stream);
+  return p.b_square ? run_by_width<true, float>(p, part, stream) : run_by_width<false, float>(p, part, stream);
 }
 
 }  // namespace sage

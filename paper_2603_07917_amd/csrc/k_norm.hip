@@ -33,7 +33,7 @@ __device__ __forceinline__ float row_sum(float x, float* lds, int w) {
   return x;
 }
 
-template <class T, int kOut, int L, int W, int S, bool kAligned>
+template <class T, int kOut, int L, int W, int S, bool kWhole>
 __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_kernel(
     const T* x, const T* residual, int M, int d, const float* __restrict__ gain, float eps, T* total, void* out,
     float* __restrict__ scales) {
@@ -50,17 +50,17 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_kernel(
 #pragma unroll
   for (int i = 0; i < S; ++i) {
     const int col = (i * L * W + in_row) * kCols;
-    load_row<T, kCols, kAligned>(s[i], x + base, col, d);
+    load_row<T, kCols, kWhole>(s[i], x + base, col, d);
     if (residual) {
       float r[kCols];
-      load_row<T, kCols, kAligned>(r, residual + base, col, d);
+      load_row<T, kCols, kWhole>(r, residual + base, col, d);
 #pragma unroll
       for (int j = 0; j < kCols; ++j) s[i][j] += r[j];
     }
   }
 #pragma unroll
   for (int i = 0; i < S; ++i) {
-    if (total) store_row<T, kCols, kAligned>(s[i], total + base, (i * L * W + in_row) * kCols, d);
+    if (total) store_row<T, kCols, kWhole>(s[i], total + base, (i * L * W + in_row) * kCols, d);
 #pragma unroll
     for (int j = 0; j < kCols; ++j) sq = fmaf(s[i][j], s[i][j], sq);
   }
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_kernel(
   for (int i = 0; i < S; ++i) {
     const int col = (i * L * W + in_row) * kCols;
     float g[kCols];
-    load_row<float, kCols, kAligned>(g, gain, col, d);
+    load_row<float, kCols, kWhole>(g, gain, col, d);
 #pragma unroll
     for (int j = 0; j < kCols; ++j) s[i][j] = s[i][j] * w * g[j];
     if constexpr (kOut == kE4M3) {
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_kernel(
         q.x = e4m3x4(s[i][0] * inv, s[i][1] * inv, s[i][2] * inv, s[i][3] * inv);
         q.y = e4m3x4(s[i][4] * inv, s[i][5] * inv, s[i][6] * inv, s[i][7] * inv);
         if (col >= d) q = make_uint2(0u, 0u);            // the padding, also of a row of NaN
-        else if (!kAligned && col + kCols > d) {
+        else if (!kWhole && col + kCols > d) {
           const uint64_t keep = ~0ull >> (8 * (col + kCols - d));
           q.x &= (uint32_t)keep;
           q.y &= (uint32_t)(keep >> 32);
@@ -95,20 +95,20 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_kernel(
         if (col % kBlock == 0) scales[(long long)(col / kBlock) * M + row] = scale;
       }
     } else if constexpr (kOut == kBF16) {
-      store_row<bf16, kCols, kAligned>(s[i], static_cast<bf16*>(out) + base, col, d);
+      store_row<bf16, kCols, kWhole>(s[i], static_cast<bf16*>(out) + base, col, d);
     } else {
-      store_row<float, kCols, kAligned>(s[i], static_cast<float*>(out) + base, col, d);
+      store_row<float, kCols, kWhole>(s[i], static_cast<float*>(out) + base, col, d);
     }
   }
   }
 }
 
-template <class T, int kOut, bool kAligned>
+template <class T, int kOut, bool kWhole>
 hipError_t norm_by_width(const T* x, const T* residual, int M, int d, const float* gain, float eps, T* total, void* out,
                          float* scales, hipStream_t stream) {
   LaunchScope scope("rms_norm_kernel", stream);
 #define SAGE_NORM(L, W, S)                                                                              \
-  rms_norm_kernel<T, kOut, L, W, S, kAligned>                                                           \
+  rms_norm_kernel<T, kOut, L, W, S, kWhole>                                                           \
       <<<min(kNormGrid, ceil_div(M, (W > 4 ? 64 * W : 256) / (L * W))), W > 4 ? 64 * W : 256, 0, stream>>>(             \
           x, residual, M, d, gain, eps, total, out, scales)
   if (d <= 128) SAGE_NORM(16, 1, 1);
@@ -124,14 +124,14 @@ hipError_t norm_by_width(const T* x, const T* residual, int M, int d, const floa
   return hipGetLastError();
 }
 
-template <class T, bool kAligned>
+template <class T, bool kWhole>
 hipError_t norm_by_out(const void* x, const void* residual, int M, int d, const float* gain, float eps, void* total,
                        void* out, Type out_type, float* scales, hipStream_t stream) {
   const T *xs = static_cast<const T*>(x), *rs = static_cast<const T*>(residual);
   T* ts = static_cast<T*>(total);
-  if (out_type == kE4M3) return norm_by_width<T, kE4M3, kAligned>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
-  if (out_type == kBF16) return norm_by_width<T, kBF16, kAligned>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
-  return norm_by_width<T, kF32, kAligned>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
+  if (out_type == kE4M3) return norm_by_width<T, kE4M3, kWhole>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
+  if (out_type == kBF16) return norm_by_width<T, kBF16, kWhole>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
+  return norm_by_width<T, kF32, kWhole>(xs, rs, M, d, gain, eps, ts, out, scales, stream);
 }
 
 // ------------------------------------------------------------- backward pass
@@ -140,7 +140,7 @@ hipError_t norm_by_out(const void* x, const void* residual, int M, int d, const 
 // sums go to a row of `part`, which norm_gain_kernel adds in a fixed order.
 constexpr int kGradGroups = 1024;                        // at most this many rows of partial sums
 
-template <class T, int L, int W, int S, bool kAligned>
+template <class T, int L, int W, int S, bool kWhole>
 __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_grad_kernel(
     const T* grad, const T* total, int M, int d, const float* __restrict__ gain, float eps, const T* grad_total,
     T* grad_x, float* __restrict__ part) {
@@ -161,13 +161,13 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_grad_kernel(
 #pragma unroll
     for (int i = 0; i < S; ++i) {
       const int col = (i * L * W + in_row) * kCols;
-      load_row<T, kCols, kAligned>(s[i], total + base, col, d);
-      load_row<T, kCols, kAligned>(dy[i], grad + base, col, d);
+      load_row<T, kCols, kWhole>(s[i], total + base, col, d);
+      load_row<T, kCols, kWhole>(dy[i], grad + base, col, d);
     }
 #pragma unroll
     for (int i = 0; i < S; ++i) {
       float g[kCols];
-      load_row<float, kCols, kAligned>(g, gain, (i * L * W + in_row) * kCols, d);
+      load_row<float, kCols, kWhole>(g, gain, (i * L * W + in_row) * kCols, d);
 #pragma unroll
       for (int j = 0; j < kCols; ++j) {
         sq = fmaf(s[i][j], s[i][j], sq);
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_grad_kernel(
     for (int i = 0; i < S; ++i) {
       const int col = (i * L * W + in_row) * kCols;
       float g[kCols], o[kCols];
-      load_row<float, kCols, kAligned>(g, gain, col, d);
+      load_row<float, kCols, kWhole>(g, gain, col, d);
 #pragma unroll
       for (int j = 0; j < kCols; ++j) {
         dg[i][j] = fmaf(dy[i][j] * s[i][j], w, dg[i][j]);
@@ -197,17 +197,17 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_grad_kernel(
       }
       if (grad_total) {
         float t[kCols];
-        load_row<T, kCols, kAligned>(t, grad_total + base, col, d);
+        load_row<T, kCols, kWhole>(t, grad_total + base, col, d);
 #pragma unroll
         for (int j = 0; j < kCols; ++j) o[j] += t[j];
       }
-      store_row<T, kCols, kAligned>(o, grad_x + base, col, d);
+      store_row<T, kCols, kWhole>(o, grad_x + base, col, d);
     }
   }
   float* mine = part + (long long)blockIdx.x * d;
   if constexpr (kRows == 1) {
 #pragma unroll
-    for (int i = 0; i < S; ++i) store_row<float, kCols, kAligned>(dg[i], mine, (i * L * W + in_row) * kCols, d);
+    for (int i = 0; i < S; ++i) store_row<float, kCols, kWhole>(dg[i], mine, (i * L * W + in_row) * kCols, d);
   } else {
 #pragma unroll
     for (int i = 0; i < S; ++i)
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(1024) norm_gain_kernel(const float* __restrict
 int norm_rows_per_group(int d) { return d <= 128 ? 16 : d <= 256 ? 8 : d <= 2048 ? 4 : 1; }
 int norm_grad_groups(int M, int d) { return min(kGradGroups, ceil_div(M, norm_rows_per_group(d))); }
 
-template <class T, bool kAligned>
+template <class T, bool kWhole>
 hipError_t norm_grad_by_width(const void* grad, const void* total, int M, int d, const float* gain, float eps,
                               const void* grad_total, void* grad_x, float* grad_gain, float* part,
                               hipStream_t stream) {
@@ -256,7 +256,7 @@ hipError_t norm_grad_by_width(const void* grad, const void* total, int M, int d,
   if (groups > 0) {
     LaunchScope scope("rms_norm_grad_kernel", stream);
 #define SAGE_NORM_GRAD(L, W, S)                                                                       \
-  rms_norm_grad_kernel<T, L, W, S, kAligned><<<groups, W > 4 ? 64 * W : 256, 0, stream>>>(            \
+  rms_norm_grad_kernel<T, L, W, S, kWhole><<<groups, W > 4 ? 64 * W : 256, 0, stream>>>(            \
       static_cast<const T*>(grad), static_cast<const T*>(total), M, d, gain, eps,                     \
       static_cast<const T*>(grad_total), static_cast<T*>(grad_x), part)
     if (d <= 128) SAGE_NORM_GRAD(16, 1, 1);
@@ -279,7 +279,7 @@ hipError_t norm_grad_by_width(const void* grad, const void* total, int M, int d,
 
 // -------------------------------------------------------------- 8-bit blocks
 // 1 x 128 blocks, as they lie: 16 lanes a block, 8 values each.
-template <class T, bool kAligned>
+template <class T, bool kWhole>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict__ x, int M, int K, int kb,
                                                             uint8_t* __restrict__ q, float* __restrict__ scales) {
   const unsigned blk = blockIdx.x * 16 + threadIdx.x / 16;   // below 2^28
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict_
   if (row >= M) return;
   const int col = b * kBlock + in_block * kCols, kp = (K + 15) & ~15;
   float v[kCols];
-  load_row<T, kCols, kAligned>(v, x + (long long)row * K, col, K);
+  load_row<T, kCols, kWhole>(v, x + (long long)row * K, col, K);
   float amax = 0.0f;
 #pragma unroll
   for (int j = 0; j < kCols; ++j) amax = fmaxf(amax, finite_mag(v[j]));
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T* __restrict_
 // one per column (the rows of the transpose). Thread (t / 16, t % 16) holds 8
 // rows x 8 columns. Transposed tiles pass through LDS as bytes, 8 rows of one
 // column at a time, and leave as whole 128-byte lines.
-template <class T, bool kSquare, bool kTranspose, bool kAligned>
+template <class T, bool kSquare, bool kTranspose, bool kWhole>
 __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* __restrict__ x, int M, int K, int kb, int mb,
                                                             uint8_t* __restrict__ q, float* __restrict__ scales) {
   constexpr int kPitch = kBlock + 8;                     // bytes between the tile's columns in LDS
@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* __restrict_
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = r0 + rg * 8 + i;
-    load_row<T, kCols, kAligned>(v[i], x + (long long)r * K, r < M ? col : K, K);
+    load_row<T, kCols, kWhole>(v[i], x + (long long)r * K, r < M ? col : K, K);
 #pragma unroll
     for (int j = 0; j < kCols; ++j) top[j] = fmaxf(top[j], finite_mag(v[i][j]));
   }
@@ -385,22 +385,22 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T* __restrict_
   }
 }
 
-template <class T, bool kAligned>
+template <class T, bool kWhole>
 hipError_t quantize_by_block(const void* xv, int M, int K, bool square, bool transpose, uint8_t* q, float* scales,
                              hipStream_t stream) {
   const T* x = static_cast<const T*>(xv);
   if (!square && !transpose) {
     LaunchScope scope("quantize_rows_kernel", stream);
     const int kb = ceil_div(K, kBlock);
-    quantize_rows_kernel<T, kAligned><<<(unsigned)(((long long)M * kb + 15) / 16), 256, 0, stream>>>(x, M, K, kb, q, scales);
+    quantize_rows_kernel<T, kWhole><<<(unsigned)(((long long)M * kb + 15) / 16), 256, 0, stream>>>(x, M, K, kb, q, scales);
     return hipGetLastError();
   }
   LaunchScope scope("quantize_tile_kernel", stream);
   const int kb = ceil_div(K, kBlock), mb = ceil_div(M, kBlock);
   const unsigned grid = (unsigned)kb * (unsigned)mb;
-  if (square && transpose) quantize_tile_kernel<T, true, true, kAligned><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
-  else if (square) quantize_tile_kernel<T, true, false, kAligned><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
-  else quantize_tile_kernel<T, false, true, kAligned><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
+  if (square && transpose) quantize_tile_kernel<T, true, true, kWhole><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
+  else if (square) quantize_tile_kernel<T, true, false, kWhole><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
+  else quantize_tile_kernel<T, false, true, kWhole><<<grid, 256, 0, stream>>>(x, M, K, kb, mb, q, scales);
   return hipGetLastError();
 }
 
@@ -421,11 +421,11 @@ hipError_t launch_rms_norm_grad(const void* grad, const void* total, Type type, 
                                 float eps, const void* grad_total, void* grad_x, float* grad_gain, void* ws,
                                 hipStream_t stream) {
   float* part = static_cast<float*>(ws);
-  const bool aligned = d % 8 == 0;
+  const bool whole = d % 8 == 0;
   if (type == kBF16)
-    return aligned ? norm_grad_by_width<bf16, true>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream)
+    return whole ? norm_grad_by_width<bf16, true>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream)
                    : norm_grad_by_width<bf16, false>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream);
-  return aligned ? norm_grad_by_width<float, true>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream)
+  return whole ? norm_grad_by_width<float, true>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream)
                  : norm_grad_by_width<float, false>(grad, total, M, d, gain, eps, grad_total, grad_x, grad_gain, part, stream);
 }
 

@@ -18,41 +18,43 @@ inline int ceil_div(int a, int b) { return a / b + (a % b != 0); }
 inline int pad16(int n) { return (n + 15) & ~15; }
 
 // ---------------------------------------------------------------------------
-// V consecutive elements of a row, as fp32. kAligned: row starts and d are
-// such that a whole vector can be loaded at once and is inside the row or
-// outside it; otherwise element by element. Columns from d on read as 0.
+// V consecutive elements of a row, as fp32. Whole vectors are loaded and stored at
+// once wherever the row starts (the address unit takes any alignment of an
+// element; rows of 1,001 bf16 values element by element took 3 to 6 times as
+// long). kWhole: d is a multiple of V, so no vector passes the row's end;
+// otherwise the last one goes by elements. Columns from d on read as 0.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float from_bits_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float from_bits_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
 
-template <class T, int V, bool kAligned>
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t uintx4;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float floatx4;
+// The same at any address of an element.
+struct __attribute__((packed, aligned(2))) Bits16 { uintx4 v; };
+struct __attribute__((packed, aligned(2))) Bits8 { uint32_t v[2]; };
+struct __attribute__((packed, aligned(4))) Floats4 { floatx4 v; };
+
+template <class T, int V, bool kWhole>
 __device__ __forceinline__ void load_row(float (&v)[V], const T* row, int col, int d) {
-  if constexpr (kAligned) {
-    if (col < d) {
-      if constexpr (sizeof(T) == 2) {
-        static_assert(V % 8 == 0, "whole 16-byte pieces");
+  if (kWhole ? col < d : col + V <= d) {
+    if constexpr (sizeof(T) == 2) {
+      static_assert(V % 8 == 0, "whole 16-byte pieces");
 #pragma unroll
-        for (int i = 0; i < V; i += 8) {
-          const uint4 u = *reinterpret_cast<const uint4*>(row + col + i);
-          v[i] = from_bits_lo(u.x), v[i + 1] = from_bits_hi(u.x);
-          v[i + 2] = from_bits_lo(u.y), v[i + 3] = from_bits_hi(u.y);
-          v[i + 4] = from_bits_lo(u.z), v[i + 5] = from_bits_hi(u.z);
-          v[i + 6] = from_bits_lo(u.w), v[i + 7] = from_bits_hi(u.w);
-        }
-      } else {
+      for (int i = 0; i < V; i += 8) {
+        const uintx4 u = reinterpret_cast<const Bits16*>(row + col + i)->v;
 #pragma unroll
-        for (int i = 0; i < V; i += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(row + col + i);
-          v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
-        }
+        for (int k = 0; k < 4; ++k) v[i + 2 * k] = from_bits_lo(u[k]), v[i + 2 * k + 1] = from_bits_hi(u[k]);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = 0.0f;
+      for (int i = 0; i < V; i += 4) {
+        const floatx4 f = reinterpret_cast<const Floats4*>(row + col + i)->v;
+        v[i] = f[0], v[i + 1] = f[1], v[i + 2] = f[2], v[i + 3] = f[3];
+      }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = col + i < d ? (float)row[col + i] : 0.0f;
+    for (int i = 0; i < V; ++i) v[i] = !kWhole && col + i < d ? (float)row[col + i] : 0.0f;
   }
 }
 
@@ -64,27 +66,25 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return p.u;
 }
 
-template <class T, int V, bool kAligned>
+template <class T, int V, bool kWhole>
 __device__ __forceinline__ void store_row(const float (&v)[V], T* row, int col, int d) {
-  if constexpr (kAligned) {
-    if (col < d) {
-      if constexpr (sizeof(T) == 2) {
-        if constexpr (V == 4) {
-          *reinterpret_cast<uint2*>(row + col) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; i += 8)
-            *reinterpret_cast<uint4*>(row + col + i) =
-                make_uint4(bf16_pair(v[i], v[i + 1]), bf16_pair(v[i + 2], v[i + 3]), bf16_pair(v[i + 4], v[i + 5]),
-                           bf16_pair(v[i + 6], v[i + 7]));
-        }
+  if (kWhole ? col < d : col + V <= d) {
+    if constexpr (sizeof(T) == 2) {
+      if constexpr (V == 4) {
+        *reinterpret_cast<Bits8*>(row + col) = Bits8{{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}};
       } else {
 #pragma unroll
-        for (int i = 0; i < V; i += 4)
-          *reinterpret_cast<float4*>(row + col + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        for (int i = 0; i < V; i += 8)
+          reinterpret_cast<Bits16*>(row + col + i)->v =
+              uintx4{bf16_pair(v[i], v[i + 1]), bf16_pair(v[i + 2], v[i + 3]), bf16_pair(v[i + 4], v[i + 5]),
+                     bf16_pair(v[i + 6], v[i + 7])};
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i += 4)
+        reinterpret_cast<Floats4*>(row + col + i)->v = floatx4{v[i], v[i + 1], v[i + 2], v[i + 3]};
     }
-  } else {
+  } else if constexpr (!kWhole) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
       if (col + i < d) row[col + i] = (T)v[i];

@@ -129,8 +129,8 @@ class PromptEncoder:
 
 def main():
     """Encodes a batch of random prompts, decides their order against a store of
-    other prompts' embeddings, and pulls each prompt towards a target of its own
-    for a few steps."""
+    other prompts' embeddings, and pulls some of them towards targets of their
+    own for a few steps."""
     from . import workloads
     torch.manual_seed(0)
     vocab, d, Q, T = 5000, 384, 256, 2000
@@ -150,12 +150,14 @@ def main():
     ids, sims, *_, order = enc.decide(store, tokens, offsets)
     print(f"decided {Q} prompts of {T} tokens: nearest similarity {sims[:, 0].mean().item():.3f}, "
           f"first served {order[:4].tolist()}")
-    target = torch.nn.functional.normalize(torch.randn(Q, d, device="cuda"), dim=1)
-    for k in range(5):
+    offsets = offsets[:25].contiguous()                  # train on the first 24
+    tokens = tokens[:int(offsets[-1])]
+    target = torch.nn.functional.normalize(torch.randn(24, d, device="cuda"), dim=1)
+    for k in range(10):
         saved = []
         e = enc.encode(tokens, offsets, saved)
         loss = (1.0 - (e * target).sum(1)).mean()
-        enc.step(enc.gradients(tokens, offsets, saved, -target / Q), 4.0)
+        enc.step(enc.gradients(tokens, offsets, saved, -target / 24), 1.0)
         print(f"step {k}: mean distance from the targets {loss.item():.4f}")
 
 
