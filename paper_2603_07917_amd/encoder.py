@@ -13,8 +13,9 @@ and each layer adds a two-layer perceptron of the normalised vector,
 with the norms' outputs, the hidden vectors and the weights in 8 bits (scales
 per block of 128) and everything between in bf16. Weights are kept in fp32, and
 `refresh` lays them out again after they change. `gradients` runs the backward
-pass, its products in 8 bits as well (a rounding counts as the identity, and a
-hidden value is on the side of the ReLU where the forward pass had it).
+pass, its products in 8 bits as well (a rounding counts as the identity, a
+hidden value is on the side of the ReLU where the forward pass had it, and a
+prompt whose vector is zero has no gradient).
 
     python -m paper_2603_07917_amd.encoder          # a small run on the GPU
 """
@@ -102,7 +103,10 @@ class PromptEncoder:
         the `encode` call that filled `saved`: {"table": [vocab, d], "layers":
         [{"gain", "w1", "b1", "w2", "b2"}, ...]}, all fp32. `add` [vocab, d] is
         a gradient of the table to add to, in place."""
-        dx, _ = sage.rms_norm_grad(grad.to(torch.bfloat16), saved[-1], self.unit, eps=FINAL_EPS)
+        # a zero vector (an empty prompt under zero biases) has no direction: 1 / |x|
+        # would be a factor of a million on its gradient
+        has = saved[-1].ne(0).any(1, keepdim=True)
+        dx, _ = sage.rms_norm_grad(torch.where(has, grad, 0.0).to(torch.bfloat16), saved[-1], self.unit, eps=FINAL_EPS)
         found = []
         for layer, (x, h) in zip(reversed(self.layers), reversed(saved[:-1])):
             dy8 = sage.quantize(dx)

@@ -91,6 +91,22 @@ def test_gradients():
         assert rel < 0.153, (name, rel)
 
 
+def test_a_prompt_without_a_direction_has_no_gradient():
+    enc = PromptEncoder(300, 96, 200, 2, seed=3)         # zero biases: an empty prompt's vector is zero
+    full, cuts = prompts(300, [20] * 24, 4)
+    target = torch.nn.functional.normalize(torch.randn(25, 96, generator=torch.Generator().manual_seed(1)), dim=1).cuda()
+    saved, with_empty = [], torch.cat([cuts, cuts[-1:]])
+    out = enc.encode(full, with_empty, saved)
+    assert int(out[24].count_nonzero()) == 0
+    got = enc.gradients(full, with_empty, saved, -target)
+    target[24] = 0.0
+    want = enc.gradients(full, with_empty, saved, -target)
+    assert torch.equal(got["table"], want["table"])
+    for a, b in zip(got["layers"], want["layers"]):
+        for k in a:
+            assert torch.equal(a[k], b[k]) and bool(torch.isfinite(a[k]).all())
+
+
 def test_descent_brings_prompts_to_their_targets():
     enc = encoder()
     tokens, offsets = prompts(300, [20] * 24, 4)
