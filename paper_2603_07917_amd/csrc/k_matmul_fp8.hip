@@ -45,11 +45,11 @@ __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
 // after.)
 __device__ __forceinline__ void load16_to_lds(const void* base, uint32_t off, uint32_t to, uint64_t mask) {
   asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
-               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane((int)to)), "s"(mask) : "memory");
+               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane((int)to)), "s"(mask) : "m0", "memory");
 }
 __device__ __forceinline__ void load4_to_lds(const void* base, uint32_t off, uint32_t to, uint64_t mask) {
   asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n\ts_mov_b64 exec, -1"
-               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane((int)to)), "s"(mask) : "memory");
+               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane((int)to)), "s"(mask) : "m0", "memory");
 }
 // LDS address of a shared array; the array counts as written by the loads from here on.
 __device__ __forceinline__ uint32_t lds_address(char* p) {

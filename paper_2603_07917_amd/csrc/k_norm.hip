@@ -15,7 +15,6 @@ namespace sage {
 namespace {
 
 constexpr int kCols = 8;                                 // consecutive columns of a lane in one step
-
 constexpr int kNormGrid = 1 << 20;                       // workgroups at most; rows past them in turns
 
 // A row takes L lanes of a wave (L = 16, 32, 64), or W whole waves (L = 64),
@@ -43,63 +42,63 @@ __global__ void __launch_bounds__(W > 4 ? 64 * W : 256) rms_norm_kernel(
   const int in_row = threadIdx.x % (L * W);
   int turn = 0;
   for (int row = blockIdx.x * kRows + (int)threadIdx.x / (L * W); row < M; row += gridDim.x * kRows, turn ^= 1) {
-  const long long base = (long long)row * d;
+    const long long base = (long long)row * d;
 
-  float s[S][kCols];
-  float sq = 0.0f;
+    float s[S][kCols];
+    float sq = 0.0f;
 #pragma unroll
-  for (int i = 0; i < S; ++i) {
-    const int col = (i * L * W + in_row) * kCols;
-    load_row<T, kCols, kWhole>(s[i], x + base, col, d);
-    if (residual) {
-      float r[kCols];
-      load_row<T, kCols, kWhole>(r, residual + base, col, d);
+    for (int i = 0; i < S; ++i) {
+      const int col = (i * L * W + in_row) * kCols;
+      load_row<T, kCols, kWhole>(s[i], x + base, col, d);
+      if (residual) {
+        float r[kCols];
+        load_row<T, kCols, kWhole>(r, residual + base, col, d);
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) s[i][j] += r[j];
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < S; ++i) {
-    if (total) store_row<T, kCols, kWhole>(s[i], total + base, (i * L * W + in_row) * kCols, d);
-#pragma unroll
-    for (int j = 0; j < kCols; ++j) sq = fmaf(s[i][j], s[i][j], sq);
-  }
-  sq = row_sum<W>(group_sum_f32<L>(sq), lds[turn], in_row / 64);
-  const float w = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(sq, (float)d) + eps));
-
-#pragma unroll
-  for (int i = 0; i < S; ++i) {
-    const int col = (i * L * W + in_row) * kCols;
-    float g[kCols];
-    load_row<float, kCols, kWhole>(g, gain, col, d);
-#pragma unroll
-    for (int j = 0; j < kCols; ++j) s[i][j] = s[i][j] * w * g[j];
-    if constexpr (kOut == kE4M3) {
-      float amax = 0.0f;
-#pragma unroll
-      for (int j = 0; j < kCols; ++j) amax = fmaxf(amax, finite_mag(s[i][j]));
-      amax = group_max_f32<16>(amax);
-      const float scale = block_scale(amax), inv = __fdiv_rn(1.0f, scale);
-      const int dp = (d + 15) & ~15;
-      if (col < dp) {
-        uint2 q;
-        q.x = e4m3x4(s[i][0] * inv, s[i][1] * inv, s[i][2] * inv, s[i][3] * inv);
-        q.y = e4m3x4(s[i][4] * inv, s[i][5] * inv, s[i][6] * inv, s[i][7] * inv);
-        if (col >= d) q = make_uint2(0u, 0u);            // the padding, also of a row of NaN
-        else if (!kWhole && col + kCols > d) {
-          const uint64_t keep = ~0ull >> (8 * (col + kCols - d));
-          q.x &= (uint32_t)keep;
-          q.y &= (uint32_t)(keep >> 32);
-        }
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out) + (long long)row * dp + col) = q;
-        if (col % kBlock == 0) scales[(long long)(col / kBlock) * M + row] = scale;
+        for (int j = 0; j < kCols; ++j) s[i][j] += r[j];
       }
-    } else if constexpr (kOut == kBF16) {
-      store_row<bf16, kCols, kWhole>(s[i], static_cast<bf16*>(out) + base, col, d);
-    } else {
-      store_row<float, kCols, kWhole>(s[i], static_cast<float*>(out) + base, col, d);
     }
-  }
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      if (total) store_row<T, kCols, kWhole>(s[i], total + base, (i * L * W + in_row) * kCols, d);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) sq = fmaf(s[i][j], s[i][j], sq);
+    }
+    sq = row_sum<W>(group_sum_f32<L>(sq), lds[turn], in_row / 64);
+    const float w = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(sq, (float)d) + eps));
+
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int col = (i * L * W + in_row) * kCols;
+      float g[kCols];
+      load_row<float, kCols, kWhole>(g, gain, col, d);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) s[i][j] = s[i][j] * w * g[j];
+      if constexpr (kOut == kE4M3) {
+        float amax = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) amax = fmaxf(amax, finite_mag(s[i][j]));
+        amax = group_max_f32<16>(amax);
+        const float scale = block_scale(amax), inv = __fdiv_rn(1.0f, scale);
+        const int dp = (d + 15) & ~15;
+        if (col < dp) {
+          uint2 q;
+          q.x = e4m3x4(s[i][0] * inv, s[i][1] * inv, s[i][2] * inv, s[i][3] * inv);
+          q.y = e4m3x4(s[i][4] * inv, s[i][5] * inv, s[i][6] * inv, s[i][7] * inv);
+          if (col >= d) q = make_uint2(0u, 0u);            // the padding, also of a row of NaN
+          else if (!kWhole && col + kCols > d) {
+            const uint64_t keep = ~0ull >> (8 * (col + kCols - d));
+            q.x &= (uint32_t)keep;
+            q.y &= (uint32_t)(keep >> 32);
+          }
+          *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out) + (long long)row * dp + col) = q;
+          if (col % kBlock == 0) scales[(long long)(col / kBlock) * M + row] = scale;
+        }
+      } else if constexpr (kOut == kBF16) {
+        store_row<bf16, kCols, kWhole>(s[i], static_cast<bf16*>(out) + base, col, d);
+      } else {
+        store_row<float, kCols, kWhole>(s[i], static_cast<float*>(out) + base, col, d);
+      }
+    }
   }
 }
 
@@ -107,9 +106,9 @@ template <class T, int kOut, bool kWhole>
 hipError_t norm_by_width(const T* x, const T* residual, int M, int d, const float* gain, float eps, T* total, void* out,
                          float* scales, hipStream_t stream) {
   LaunchScope scope("rms_norm_kernel", stream);
-#define SAGE_NORM(L, W, S)                                                                              \
-  rms_norm_kernel<T, kOut, L, W, S, kWhole>                                                           \
-      <<<min(kNormGrid, ceil_div(M, (W > 4 ? 64 * W : 256) / (L * W))), W > 4 ? 64 * W : 256, 0, stream>>>(             \
+#define SAGE_NORM(L, W, S)                                                                                  \
+  rms_norm_kernel<T, kOut, L, W, S, kWhole>                                                                 \
+      <<<min(kNormGrid, ceil_div(M, (W > 4 ? 64 * W : 256) / (L * W))), W > 4 ? 64 * W : 256, 0, stream>>>( \
           x, residual, M, d, gain, eps, total, out, scales)
   if (d <= 128) SAGE_NORM(16, 1, 1);
   else if (d <= 256) SAGE_NORM(32, 1, 1);
@@ -135,7 +134,7 @@ hipError_t norm_by_out(const void* x, const void* residual, int M, int d, const 
 }
 
 // ------------------------------------------------------------- backward pass
-// A workgroup takes kGroup = 4 / W rows at a time and every gridDim.x-th such
+// A workgroup takes kRows rows at a time and every gridDim.x-th such
 // group, and keeps its columns' sums of dy s w in registers; each workgroup's
 // sums go to a row of `part`, which norm_gain_kernel adds in a fixed order.
 constexpr int kGradGroups = 1024;                        // at most this many rows of partial sums
@@ -255,9 +254,9 @@ hipError_t norm_grad_by_width(const void* grad, const void* total, int M, int d,
   const int groups = norm_grad_groups(M, d);
   if (groups > 0) {
     LaunchScope scope("rms_norm_grad_kernel", stream);
-#define SAGE_NORM_GRAD(L, W, S)                                                                       \
-  rms_norm_grad_kernel<T, L, W, S, kWhole><<<groups, W > 4 ? 64 * W : 256, 0, stream>>>(            \
-      static_cast<const T*>(grad), static_cast<const T*>(total), M, d, gain, eps,                     \
+#define SAGE_NORM_GRAD(L, W, S)                                                           \
+  rms_norm_grad_kernel<T, L, W, S, kWhole><<<groups, W > 4 ? 64 * W : 256, 0, stream>>>(  \
+      static_cast<const T*>(grad), static_cast<const T*>(total), M, d, gain, eps,         \
       static_cast<const T*>(grad_total), static_cast<T*>(grad_x), part)
     if (d <= 128) SAGE_NORM_GRAD(16, 1, 1);
     else if (d <= 256) SAGE_NORM_GRAD(32, 1, 1);
