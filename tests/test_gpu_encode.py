@@ -124,6 +124,29 @@ def test_embed_grad(T, Q, V, d, gtype, mean, held):
     close(got, want, mag * (n + 6) * U32)
 
 
+# Where the order of the tokens is found in another way, and texts that put all of it on few places.
+ORDERS = [(8192, 262144, "text"), (8193, 262144, "text"), (8193, 262145, "text"), (8193, 1, "text"), (131072, 262144, "text"),
+          (131073, 262144, "text"), (16385, 257, "text"), (60001, 70000, "one"), (60001, 70000, "none"),
+          (40000, 200000, "multiples"), (30000, 255, "last")]
+
+
+@pytest.mark.parametrize("T,V,kind", ORDERS)
+@pytest.mark.parametrize("Q", [0, 70])
+def test_embed_grad_orders(T, V, kind, Q):
+    tok = {"text": lambda: tokens_like(T, V, T, pad=0.1), "one": lambda: torch.full((T,), V - 1, dtype=torch.int32),
+           "none": lambda: torch.where(torch.arange(T) % 2 == 0, -1, V).to(torch.int32),
+           "multiples": lambda: (torch.randint(0, V // 256, (T,), generator=gen(T)) * 256).to(torch.int32),
+           "last": lambda: torch.where(torch.arange(T) % 5 == 0, V, V - 1).to(torch.int32)}[kind]()
+    off = None
+    if Q:                                                # tokens before the first prompt and behind the last one
+        off = cut(T - 300, Q, T)
+        off = (off + 100).to(torch.int32)
+    g = torch.randn(Q or T, 24, generator=gen(5)).cuda()
+    want, mag, n = ref.embed_grad(tok, g, V, 1.0, off, Q > 0, None)
+    got = sage.embed_grad(tok.cuda(), g, V, offsets=None if off is None else off.cuda(), mean=Q > 0)
+    close(got, want, mag * (n + 6) * U32)
+
+
 def test_embed_grad_repeats_bit_for_bit_and_is_the_transpose():
     T, Q, V, d = 40000, 50, 700, 96
     tok, off = tokens_like(T, V, 1, pad=0.05).cuda(), cut(T, Q, 2).cuda()
