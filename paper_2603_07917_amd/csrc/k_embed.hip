@@ -47,28 +47,54 @@ __global__ void __launch_bounds__(256) embed_tokens_kernel(const int32_t* __rest
   }
 }
 
-// Prompt of each token (-1: none), for the kernels below, which ask several
-// times; and the rows of prompts without tokens. A workgroup takes 2,048 tokens
-// and searches between their first and last prompts.
-constexpr int kPromptTokens = 2048;
+// The prompt that token i of offsets[lo] <= i < offsets[hi] is in.
 __device__ __forceinline__ int last_at_most(const int32_t* __restrict__ offsets, int lo, int hi, int i) {
-  while (hi - lo > 1) {                                  // offsets[lo] <= i < offsets[hi]
+  while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (offsets[mid] <= i) lo = mid; else hi = mid;
   }
   return lo;
 }
+// Prompt of each token (-1: none), for the kernels below, which ask several
+// times. Bound by the latency of dependent loads: a workgroup takes 2,048 tokens,
+// whose first and last prompts each wave finds in steps of 64 probes, and a
+// thread searches between them for eight tokens at a time.
+constexpr int kPromptTokens = 2048;
 __global__ void __launch_bounds__(256) prompt_of_kernel(const int32_t* __restrict__ offsets, int T, int Q,
                                                         int32_t* __restrict__ prompt) {
+  constexpr int kTake = kPromptTokens / 256;
   const int first = blockIdx.x * kPromptTokens, last = min(first + kPromptTokens, T) - 1;
   const int begin = offsets[0], end = offsets[Q];
-  int lo = 0, hi = Q;
+  int lo = 0, hi = 1;                                    // the prompts between which the tokens' are
   if (begin <= last && first < end) {
-    lo = last_at_most(offsets, 0, Q, max(first, begin));
-    hi = last_at_most(offsets, 0, Q, min(last, end - 1)) + 1;
+    const int want[2] = {max(first, begin), min(last, end - 1)};
+    int l[2] = {0, 0}, h[2] = {Q, Q};
+    while (h[0] - l[0] > 1 || h[1] - l[1] > 1) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int step = (h[k] - l[k] + 63) / 64, at = l[k] + (int)lane_id() * step;
+        const int n = (int)__popcll(__ballot(at < h[k] && offsets[at] <= want[k]));
+        l[k] += max(n - 1, 0) * step;                    // lane 0's is at most the token, if the offsets ascend
+        h[k] = min(l[k] + step, h[k]);
+      }
+    }
+    lo = l[0], hi = l[1] + 1;
   }
-  for (int i = first + (int)threadIdx.x; i <= last; i += 256)
-    prompt[i] = i >= begin && i < end ? last_at_most(offsets, lo, hi, i) : -1;
+  int l[kTake], h[kTake];
+#pragma unroll
+  for (int u = 0; u < kTake; ++u) l[u] = lo, h[u] = hi;
+  for (int span = hi - lo; span > 1; span = (span + 1) / 2) {
+#pragma unroll
+    for (int u = 0; u < kTake; ++u) {
+      const int mid = (l[u] + h[u]) >> 1;                // l itself where the search is over
+      if (offsets[mid] <= first + u * 256 + (int)threadIdx.x) l[u] = mid; else h[u] = mid;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kTake; ++u) {
+    const int i = first + u * 256 + (int)threadIdx.x;
+    if (i <= last) prompt[i] = i >= begin && i < end ? l[u] : -1;
+  }
 }
 
 // ------------------------------------------------------------ list of items

@@ -65,6 +65,15 @@ def test_embed_prompts(T, Q, V, d, ttype, otype, mean):
     close(got, want, mag * (n + 4) * U32 + want.abs() * UNIT[otype])
 
 
+@pytest.mark.parametrize("T,Q", [(6000, 63), (6000, 64), (6000, 65), (9000, 4097), (10000, 300000), (4097, 1), (8192, 2048)])
+@pytest.mark.parametrize("outside", [0, 50])
+def test_embed_finds_the_prompts(T, Q, outside):
+    off = (cut(T - 2 * outside, Q, T) + outside).to(torch.int32)   # tokens before the first prompt and behind the last
+    tok = torch.zeros(T, dtype=torch.int32, device="cuda")
+    got = sage.embed(tok, torch.ones(1, 264, device="cuda"), offsets=off.cuda())
+    assert torch.equal(got.cpu(), (off[1:] - off[:-1]).float()[:, None].expand(-1, 264))
+
+
 def test_embed_empty_prompts_and_no_valid_token():
     table = torch.ones(4, 24, device="cuda")
     tok = torch.tensor([-1, 9, 2, 3], dtype=torch.int32, device="cuda")
