@@ -191,10 +191,10 @@ struct Finish {
   float scale;
   bool mean;
   int d;
+  // Columns c to c + V - 1.
   template <int V, bool kWhole>
-  __device__ __forceinline__ void load_add(float (&held)[V], int seg, int piece) const {
+  __device__ __forceinline__ void load_add_at(float (&held)[V], int seg, int c) const {
     const float* row = add + (long long)seg * d;
-    const int c = (piece * kGroup + (int)lane_id() % kGroup) * V;
     if (kStream && c + V <= d) {
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
@@ -202,17 +202,16 @@ struct Finish {
         held[j] = q[0], held[j + 1] = q[1], held[j + 2] = q[2], held[j + 3] = q[3];
       }
     } else {
-      load_cols<V, kWhole>(held, row, piece, d);
+      load_row<float, V, kWhole>(held, row, c, d);
     }
   }
   template <int V, bool kWhole>
-  __device__ __forceinline__ void write(const float (&acc)[V], const float (&held)[V], int count, int seg, int piece) const {
+  __device__ __forceinline__ void write_at(const float (&acc)[V], const float (&held)[V], int count, int seg, int at) const {
     const float c = mean && count > 0 ? __fdiv_rn(scale, (float)count) : scale;
     float v[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] = add ? fmaf(acc[j], c, held[j]) : acc[j] * c;
     O* row = out + (long long)seg * d;
-    const int at = (piece * kGroup + (int)lane_id() % kGroup) * V;
     if constexpr (kStream) {
       if (at + V <= d) {
 #pragma unroll
@@ -220,7 +219,16 @@ struct Finish {
         return;
       }
     }
-    store_cols<O, V, kWhole>(v, row, piece, d);
+    store_row<O, V, kWhole>(v, row, at, d);
+  }
+  // A lane's columns of a piece.
+  template <int V, bool kWhole>
+  __device__ __forceinline__ void load_add(float (&held)[V], int seg, int piece) const {
+    load_add_at<V, kWhole>(held, seg, (piece * kGroup + (int)lane_id() % kGroup) * V);
+  }
+  template <int V, bool kWhole>
+  __device__ __forceinline__ void write(const float (&acc)[V], const float (&held)[V], int count, int seg, int piece) const {
+    write_at<V, kWhole>(acc, held, count, seg, (piece * kGroup + (int)lane_id() % kGroup) * V);
   }
 };
 
@@ -340,16 +348,26 @@ __device__ __forceinline__ void sum_chunks(const Items& items, const T* __restri
 }
 
 // The segments that cross chunks: 16 lanes for each (chunk where one begins,
-// piece) add its partial sums in order. One of more than 16 further chunks is
+// piece) add its partial sums in order. One of 16 further chunks or more is
 // left to the whole workgroup, whose 16 groups take every 16th chunk, four at a
-// time.
+// time; and where it also covers the first chunks of the next kHelpers
+// workgroups, those take a share of its columns each (a prompt of 714,585 tokens, 768
+// columns, 4,963 chunks: 150 us by one workgroup a piece, 45 by eight).
+constexpr int kHelpers = 8;
 template <class F, int V, bool kWhole>
 __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid, Partials part, F fin) {
   __shared__ float sums[16][kGroup * V];
   __shared__ int counts[16];
   __shared__ int long_run[16];
+  __shared__ int run_start;
   const int l = threadIdx.x % kGroup, g = threadIdx.x / kGroup;
   const int piece = blockIdx.x / grid.rows(), c0 = blockIdx.x % grid.rows() * 16;
+  auto head_at = [&](int c) { return c >= 0 && c < grid.chunks ? part.head[c] : -1; };
+  // The segment that this workgroup may help with: it covers c0 and, since kHelpers
+  // workgroups' first chunks are its, also the one 4 workgroups on or back.
+  const int helped = head_at(c0);
+  const bool may_help = helped >= 0 && (head_at(c0 + kHelpers / 2 * 16) == helped || head_at(c0 - kHelpers / 2 * 16) == helped);
+  if (threadIdx.x == 0) run_start = -1;
   {
     const int c = c0 + g;
     const int seg = c < grid.chunks ? part.tail[c] : -1;
@@ -388,6 +406,7 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
   for (int s = 0; s < 16; ++s) {
     if (!long_run[s]) continue;                          // the same for all threads
     const int c = c0 + s, seg = part.tail[c];
+    if (head_at(c0 + kHelpers * 16) == seg) continue;    // left to the helpers
     float acc[V] = {};
     int count = 0;
     if (g == 0) {
@@ -432,6 +451,66 @@ __global__ void __launch_bounds__(256) segment_join_kernel(int d, ChunkGrid grid
     }
     __syncthreads();
   }
+  if (!may_help) return;                                 // the same for all threads
+  {
+    const int c = c0 - kHelpers * 16 + (int)threadIdx.x;   // its first chunk's workgroup is at most kHelpers back
+    if (c >= 0 && c < c0 && part.tail[c] == helped) run_start = c;
+  }
+  __syncthreads();
+  const int start = run_start, share = (c0 - start / 16 * 16) / 16 - 1;
+  if (start < 0 || head_at(start / 16 * 16 + kHelpers * 16) != helped) return;
+  // Share `share` of the piece's columns, 4 a lane, for every kGroups-th chunk.
+  constexpr int kLanes = kGroup * V / kHelpers / 4, kGroups = 256 / kLanes;
+  const int hl = threadIdx.x % kLanes, hg = threadIdx.x / kLanes;
+  const int col = piece * kGroup * V + (share * kLanes + hl) * 4;
+  float acc[4] = {};
+  int count = 0;
+  if (hg == 0) {
+    load_row<float, 4, kWhole>(acc, part.sum + (2LL * start + 1) * d, col, d);
+    count = part.count[2LL * start + 1];
+  }
+  bool more = true;
+  for (int k0 = start + 1; more && k0 < grid.chunks; k0 += kGroups * kTurn) {
+    float v[kTurn][4];
+    int n[kTurn];
+    bool in[kTurn];
+#pragma unroll
+    for (int u = 0; u < kTurn; ++u) {
+      const int k = min(k0 + u * kGroups + hg, grid.chunks - 1);
+      load_row<float, 4, kWhole>(v[u], part.sum + 2LL * k * d, col, d);
+      n[u] = part.count[2LL * k];
+      in[u] = k == k0 + u * kGroups + hg && part.head[k] == helped;
+    }
+    more = __syncthreads_and(in[kTurn - 1]);
+#pragma unroll
+    for (int u = 0; u < kTurn; ++u) {
+      count += in[u] ? n[u] : 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] += in[u] ? v[u][j] : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int o = kLanes; o < 64; o <<= 1) {
+    count += __shfl_xor(count, o, 64);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], o, 64);
+  }
+  const int w = threadIdx.x / 64;
+  if (threadIdx.x % 64 < kLanes) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[w][hl * 4 + j] = acc[j];
+    if (hl == 0) counts[w] = count;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x >= kLanes) return;
+  for (int i = 1; i < 4; ++i) {
+    count += counts[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += sums[i][hl * 4 + j];
+  }
+  float held[4] = {};
+  if (fin.add) fin.template load_add_at<4, kWhole>(held, helped, col);
+  fin.template write_at<4, kWhole>(acc, held, count, helped, col);
 }
 
 // Prompts: the chunks' sums, and (workgroups behind them) zeros for the prompts
@@ -495,29 +574,29 @@ __global__ void __launch_bounds__(kGroups * kGroup) prompt_whole_kernel(PromptIt
 }
 
 // Tokens: the chunks' sums, and (workgroups behind them) the rows of tokens
-// that the list does not have, zeros or `add`: 128 rows a workgroup, 32 a wave,
-// whose lane i finds the first item of its token i by a binary search.
+// that the list does not have, zeros or `add`: `take` (at most 32) a wave, whose
+// lane i finds the first item of its token i by a binary search.
 template <bool kAdd, class T, int V, bool kWhole>
 __global__ void __launch_bounds__(256) token_sum_kernel(SortedItems items, const T* __restrict__ src, int d, ChunkGrid grid,
-                                                        unsigned sum_groups, Partials part, Finish<float, true> fin) {
+                                                        unsigned sum_groups, int take, Partials part,
+                                                        Finish<float, true> fin) {
   if (blockIdx.x < sum_groups) {
     const int2 at = grid.at(blockIdx.x, sum_groups);
     if (at.x >= 0) sum_chunks<kAdd, SortedItems, T, Finish<float, true>, V, kWhole>(items, src, d, grid, at.x, at.y, part, fin);
     return;
   }
-  constexpr int kTake = 32;
   const int lane = (int)lane_id();
-  const long long first = ((long long)(blockIdx.x - sum_groups) * 4 + threadIdx.x / 64) * kTake;
+  const long long first = ((long long)(blockIdx.x - sum_groups) * 4 + threadIdx.x / 64) * take;
   if (first >= items.V) return;
   const int v0 = (int)first;
   int lo = 0, hi = items.T;
-  const uint32_t want = (uint32_t)min(v0 + min(lane, kTake), items.V);
+  const uint32_t want = (uint32_t)min(v0 + min(lane, take), items.V);
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
     if (items.keys[mid] >= want) hi = mid; else lo = mid + 1;
   }
   const int next = __shfl_down(lo, 1, 64);
-  uint64_t missing = __ballot(lane < kTake && v0 + lane < items.V && lo == next);
+  uint64_t missing = __ballot(lane < take && v0 + lane < items.V && lo == next);
   while (missing) {
     const int v = v0 + __builtin_ctzll(missing);
     missing &= missing - 1;
@@ -556,17 +635,22 @@ __device__ __forceinline__ uint32_t token_key(const PromptItems& p, int i) {
 }
 
 // kFirst: the keys come from the tokens, and (mean) each prompt's valid tokens
-// are counted: once per wave and prompt, as one prompt may have them all.
+// are counted: once per wave and prompt, and once per workgroup where its tokens are
+// of one prompt (which may have them all: 1M additions / 64 to one place are 90 us).
 template <bool kFirst>
 __global__ void __launch_bounds__(kSortThreads) token_count_kernel(PromptItems prompts, const uint32_t* __restrict__ keys,
                                                                    int T, int shift, int tiles,
                                                                    uint32_t* __restrict__ hist, int32_t* __restrict__ valid) {
   __shared__ uint32_t cnt[kSortBins];
+  __shared__ int all_valid;
   for (int b = threadIdx.x; b < kSortBins; b += kSortThreads) cnt[b] = 0;
+  if (threadIdx.x == 0) all_valid = 0;
+  const int first = blockIdx.x * kSortTile, end = min(first + kSortTile, T);
+  const int one = kFirst && valid && prompts.prompt[first] == prompts.prompt[end - 1] ? prompts.prompt[first] : -1;
   __syncthreads();
 #pragma unroll
   for (int it = 0; it < kSortItems; ++it) {
-    const int i = blockIdx.x * kSortTile + it * kSortThreads + threadIdx.x;
+    const int i = first + it * kSortThreads + threadIdx.x;
     uint32_t k = 0;
     if (i < T) {
       k = kFirst ? token_key(prompts, i) : keys[i];
@@ -578,10 +662,14 @@ __global__ void __launch_bounds__(kSortThreads) token_count_kernel(PromptItems p
       while (left) {
         const int q0 = __builtin_amdgcn_readlane(q, __builtin_ctzll(left));
         const uint64_t same = __ballot(q == q0);
-        if (lane_id() == 0) atomicAdd(&valid[q0], (int)__popcll(same));
+        if (lane_id() == 0) atomicAdd(one >= 0 ? &all_valid : &valid[q0], (int)__popcll(same));
         left &= ~same;
       }
     }
+  }
+  if (kFirst && one >= 0) {
+    __syncthreads();
+    if (threadIdx.x == 0) atomicAdd(&valid[one], all_valid);
   }
   __syncthreads();
   for (int b = threadIdx.x; b < kSortBins; b += kSortThreads) hist[(size_t)b * tiles + blockIdx.x] = cnt[b];
@@ -703,52 +791,62 @@ __global__ void __launch_bounds__(256) token_rank_kernel(PromptItems items, cons
                                                          uint32_t* __restrict__ keys_out, uint32_t* __restrict__ rows_out,
                                                          int32_t* __restrict__ valid) {
   __shared__ __attribute__((aligned(16))) uint32_t keys[kRankTokens];
-  __shared__ uint16_t before[kRankTokens + 1];           // valid tokens before each (of those in prompts)
-  __shared__ int wave_sum[4];
+  __shared__ uint64_t some[kRankTokens / 64 + 1];        // bits of the valid tokens (of those in prompts)
+  __shared__ int before[kRankTokens / 64 + 1];           // how many there are before each 64
   const int T = items.T, V = items.V, lane = (int)lane_id(), w = threadIdx.x / 64;
   const int begin = offsets ? max(offsets[0], 0) : 0, end = offsets ? min(offsets[Q], T) : T;
   const int padded = (T + 63) & ~63;
-  for (int i = threadIdx.x; i < padded; i += 256) {
-    const int id = i < T && i >= begin && i < end ? items.tokens[i] : -1;
-    keys[i] = i >= T ? 0xFFFFFFFFu : (unsigned)id < (unsigned)V ? (uint32_t)id : (uint32_t)V;
+  for (int i0 = threadIdx.x; i0 < padded; i0 += 256 * 8) {
+    int id[8];                                           // in flight together
+#pragma unroll
+    for (int u = 0; u < 8; ++u) id[u] = items.tokens[min(i0 + u * 256, T - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + u * 256;
+      const bool in = i >= begin && i < end && (unsigned)id[u] < (unsigned)V;
+      const uint64_t bits = __ballot(in);
+      if (i >= padded) continue;                         // the same for the wave
+      keys[i] = i >= T ? 0xFFFFFFFFu : in ? (uint32_t)id[u] : (uint32_t)V;
+      if (lane == 0) some[i / 64] = bits;
+    }
   }
+  if (threadIdx.x == 0) some[padded / 64] = 0;
   __syncthreads();
-  if (valid) {
-    const int per = padded / 256 + (padded % 256 != 0), i0 = threadIdx.x * per;
-    int mine = 0;
-    for (int i = i0; i < min(i0 + per, T); ++i) mine += keys[i] < (uint32_t)V;
-    int incl = mine;
+  if (valid && w == 0) {
+    const int i = 2 * lane, n = padded / 64;
+    const int v0 = i < n ? (int)__popcll(some[i]) : 0, v1 = i + 1 < n ? (int)__popcll(some[i + 1]) : 0;
+    int incl = v0 + v1;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int y = __shfl_up(incl, o, 64);
       if (lane >= o) incl += y;
     }
-    if (lane == 63) wave_sum[w] = incl;
-    __syncthreads();
-    int run = incl - mine;
-    for (int k = 0; k < w; ++k) run += wave_sum[k];
-    for (int i = i0; i < min(i0 + per, T); ++i) {
-      before[i] = (uint16_t)run;
-      run += keys[i] < (uint32_t)V;
-    }
-    if (i0 < T && i0 + per >= T) before[T] = (uint16_t)run;
-    __syncthreads();
+    before[i] = incl - v0 - v1;
+    before[i + 1] = incl - v1;
+    if (lane == 63) before[kRankTokens / 64] = incl;
   }
+  __syncthreads();
+  auto valid_before = [&](int i) { return before[i / 64] + (int)__popcll(some[i / 64] & ((1ull << (i & 63)) - 1ull)); };
   const int i = blockIdx.x * 16 + threadIdx.x / 16, part = threadIdx.x % 16;
   const uint32_t key = keys[min(i, T - 1)];
   const int own = blockIdx.x * 16 / 64 * 64;             // the 64 keys that hold the workgroup's tokens
   int place = 0;
-  for (int j = 0; j < padded; j += 64) {
-    const uint4 k = *reinterpret_cast<const uint4*>(keys + j + part * 4);
-    if (j < own) {
-      place += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
-    } else if (j > own) {
-      place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
-    } else {
-      const int at = j + part * 4;
-      place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
-      place += (k.x == key && at < i) + (k.y == key && at + 1 < i) + (k.z == key && at + 2 < i) + (k.w == key && at + 3 < i);
-    }
+  auto four = [&](int j) { return *reinterpret_cast<const uint4*>(keys + j + part * 4); };
+#pragma unroll 8
+  for (int j = 0; j < own; j += 64) {
+    const uint4 k = four(j);
+    place += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+  }
+  {
+    const uint4 k = four(own);
+    const int at = own + part * 4;
+    place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+    place += (k.x == key && at < i) + (k.y == key && at + 1 < i) + (k.z == key && at + 2 < i) + (k.w == key && at + 3 < i);
+  }
+#pragma unroll 8
+  for (int j = own + 64; j < padded; j += 64) {
+    const uint4 k = four(j);
+    place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
   }
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) place += __shfl_xor(place, o, 16);
@@ -758,8 +856,8 @@ __global__ void __launch_bounds__(256) token_rank_kernel(PromptItems items, cons
   keys_out[place] = key;
   rows_out[place] = offsets ? (uint32_t)max(q, 0) : (uint32_t)i;
   if (valid && q >= 0 && key < (uint32_t)V) {
-    const int b = max(offsets[q], 0), e = min(offsets[q + 1], T);
-    if (before[i] == before[b]) valid[q] = (int)before[e] - (int)before[b];
+    const int b = max(offsets[q], 0), e = max(b, min(offsets[q + 1], T));
+    if (valid_before(i) == valid_before(b)) valid[q] = valid_before(e) - valid_before(b);
   }
 }
 
@@ -770,12 +868,18 @@ __global__ void __launch_bounds__(256) clear_kernel(int32_t* __restrict__ p, int
 
 // ------------------------------------------------------------------- plans
 // Items per chunk: about 8,192 waves (eight per SIMD) over all chunks and
-// pieces, in whole groups of 16, 32 at least (65,000 tokens of 768 columns with 16:
-// the join of the most frequent token's 375 partial sums 17 us, with 32 10).
+// pieces, in whole groups of 16. 32 at least (65,000 tokens of 768 columns with 16:
+// the join of the most frequent token's 375 partial sums 17 us, with 32 10), but 16
+// for few tokens, where a chunk's serial work is what is waited for (gradient of
+// 6,347 tokens, 3,099 x 768: the sums 22 us with 32, 15 with 16).
 int chunk_items(int T, int pieces) {
   const long long want = (long long)T * pieces / 32768;
-  return (int)min(1024LL, max(32LL, (want + 15) / 16 * 16));
+  return (int)min(1024LL, max(T <= kRankTokens ? 16LL : 32LL, (want + 15) / 16 * 16));
 }
+// Rows without tokens per wave: about 16,384 waves (4 tokens, 6,401 x 1,024: with 32
+// rows 25 us, with 2 10; 65,000 tokens, 50,021 x 768: 32 rows 62 us, 4 rows 53, and
+// 131,072 x 1,024 with add: 390 and, with 8 rows, 379).
+int fill_rows(int V) { return min(32, max(2, ceil_div(V, 16384))); }
 int piece_count(int d, int vec) { return ceil_div(d, kGroup * vec); }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -964,12 +1068,13 @@ hipError_t embed_grad_with(const int32_t* tokens, int T_, const void* grad, int 
   const PartialLayout pl = partial_layout(T_, d, kVec);
   const Partials part = partials_at(base + l.part, pl);
   const unsigned groups = T_ > 0 ? (unsigned)pl.grid.groups() : 0;
-  const unsigned fill = add != out ? (unsigned)ceil_div(V, 128) : 0;   // in place, rows with no token stay as they are
+  const int take = fill_rows(V);
+  const unsigned fill = add != out ? (unsigned)ceil_div(V, 4 * take) : 0;   // in place, rows with no token stay as they are
   if (groups + fill > 0) {
     LaunchScope scope("token_sum_kernel", stream);
     const T* src = static_cast<const T*>(grad);
-    if (add) token_sum_kernel<true, T, kVec, kWhole><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
-    else token_sum_kernel<false, T, kVec, kWhole><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, part, fin);
+    if (add) token_sum_kernel<true, T, kVec, kWhole><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, take, part, fin);
+    else token_sum_kernel<false, T, kVec, kWhole><<<groups + fill, 256, 0, stream>>>(items, src, d, pl.grid, groups, take, part, fin);
     if ((e = hipGetLastError()) != hipSuccess || T_ == 0) return e;
   }
   if (T_ == 0) return hipSuccess;

@@ -65,6 +65,19 @@ def test_embed_prompts(T, Q, V, d, ttype, otype, mean):
     close(got, want, mag * (n + 4) * U32 + want.abs() * UNIT[otype])
 
 
+# Sums of prompts that cover from under 16 to thousands of chunks, from one place or another in them.
+@pytest.mark.parametrize("lengths", [[100000], [4000, 4200, 4700, 5100, 30000], [37, 1, 0, 9000, 513, 16, 50000, 4096], [520, 4130, 4640, 4100, 3]])
+@pytest.mark.parametrize("d,ttype", [(264, F32), (1001, BF16), (520, BF16), (70, F32)])
+def test_embed_long_prompts(lengths, d, ttype):
+    off = torch.tensor([0] + lengths).cumsum(0).to(torch.int32)
+    T = int(off[-1])
+    tok, table = tokens_like(T, 300, T + d, pad=0.1), torch.randn(300, d, generator=gen(d)).to(ttype).cuda()
+    want, mag, n = ref.embed(tok, table, 0.75, off, True)
+    got = sage.embed(tok.cuda(), table, scale=0.75, offsets=off.cuda(), mean=True, dtype=F32)
+    close(got, want, mag * (n + 4) * U32)
+    assert torch.equal(sage.embed(tok.cuda(), table, scale=0.75, offsets=off.cuda(), mean=True, dtype=F32), got)
+
+
 @pytest.mark.parametrize("T,Q", [(6000, 63), (6000, 64), (6000, 65), (9000, 4097), (10000, 300000), (4097, 1), (8192, 2048)])
 @pytest.mark.parametrize("outside", [0, 50])
 def test_embed_finds_the_prompts(T, Q, outside):
