@@ -17,6 +17,14 @@
 // Bound by the gather. Text repeats its tokens (and a gradient its prompts), so
 // each XCD takes its own columns: the 256-byte pieces of eight times as many
 // rows stay in its L2.
+//
+// Measured (kernels alone): 1,048,576 tokens of 16,384 prompts x 1,024 bf16: 183 us
+// of sums, 11.7 TB/s of gathered rows, 17 us of joins, 6 us of prompts. 714,585
+// tokens of one prompt x 768: 92 us, 12 TB/s. Gradient of 65,000 tokens, 50,021 x
+// 768: 42 us of sums for 254 MB that it must move (6.0 TB/s), 27 us of order in six
+// launches, 12 us of joins. Gradient of 524,288 tokens of 4,096 prompts, 131,072 x
+// 1,024 with add: 380 us of sums (1.09 GB of table at 2.9 TB/s beside 2.1 GB of
+// gathered gradients: their times add up, as both pass through the L2s).
 #include <type_traits>
 
 #include "sage_encode.hpp"
@@ -29,7 +37,8 @@ constexpr int kGroup = 16;                               // lanes per row piece
 constexpr int kTurn = 8;                                 // rows in flight per lane group
 
 // ------------------------------------------------------- lookup per token
-// Each thread copies pieces of 8 columns; a workgroup owns kRows tokens.
+// Each thread copies pieces of 8 columns; a workgroup owns `rows` tokens. Bound by
+// the memory (rows read and written once).
 template <class T, class O, bool kWhole>
 __global__ void __launch_bounds__(256) embed_tokens_kernel(const int32_t* __restrict__ tokens, int T_, const T* __restrict__ table,
                                                            int V, int d, int rows, float scale, O* __restrict__ out) {
@@ -531,7 +540,8 @@ __global__ void __launch_bounds__(256) prompt_sum_kernel(PromptItems items, cons
 }
 
 // Few tokens: a workgroup per prompt and piece, whose kGroups lane groups take every
-// kGroups-th token. One launch, no partial sums in memory.
+// kGroups-th token. One launch, no partial sums in memory; bound by the latency of
+// two dependent loads and the launch (211 tokens of one prompt x 768: 7.3 us).
 template <int kGroups, class T, class O, int V, bool kWhole>
 __global__ void __launch_bounds__(kGroups * kGroup) prompt_whole_kernel(PromptItems items, const int32_t* __restrict__ offsets,
                                                                         const T* __restrict__ src, int d, int pieces,
@@ -621,7 +631,9 @@ __global__ void __launch_bounds__(256) token_sum_kernel(SortedItems items, const
 // below 2^bits; a token outside [0, V) has key V) with the row that each
 // brings: its position, or its prompt. Digits of up to 9 bits; each pass
 // counts per tile, scans, and scatters, a wave ranking its own quarter of a
-// tile with ballots.
+// tile with ballots. Bound by its launches (65,000 tokens: 4.9, 3.6 and 4.9 us a
+// digit); one launch whose 256 workgroups each place the tokens of one remainder
+// took 129 us, as every one of them reads the whole list.
 constexpr int kSortBits = 9;
 constexpr int kSortBins = 1 << kSortBits;
 constexpr int kSortThreads = 256;
@@ -785,7 +797,8 @@ __global__ void __launch_bounds__(kSortThreads) token_scatter_kernel(
 // number of keys below its own, and of equal ones before it. A workgroup places 16
 // tokens, 16 threads each, against all keys in LDS; it finds their prompts, and
 // the first valid token of a prompt writes the number of its valid tokens (from a
-// prefix count).
+// prefix count). Bound by the comparisons, T^2 of them: 6,347 tokens 10 us, 71 tokens
+// 4; the sort takes 27 us at 8,193.
 constexpr int kRankTokens = 8192;
 __global__ void __launch_bounds__(256) token_rank_kernel(PromptItems items, const int32_t* __restrict__ offsets, int Q,
                                                          uint32_t* __restrict__ keys_out, uint32_t* __restrict__ rows_out,
