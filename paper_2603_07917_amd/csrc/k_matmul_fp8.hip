@@ -674,10 +674,13 @@ Plan plan_matmul(int M, int N, int K, bool fast) {
   // quarters of the CUs on (16,384 x 4,096 x 8,192: 734 us with 128, 533 with 256).
   pl.tile = fast && big >= 192 ? 256 : 128;
   const long long tiles = (long long)ceil_div(M, pl.tile) * ceil_div(N, pl.tile);
-  // Two workgroups a CU, of 4 blocks of the sum at least (4,096 x 1,024 x 16,384,
-  // exact, 256 tiles: 250 us in one split, 201 with the join in two).
+  // As many as the chip holds at a time (4,096 x 1,024 x 16,384, exact, 256 tiles: 250 us in
+  // one split, 201 with the join in two), of 8 blocks of the sum at least (1,180 x 2,113 x
+  // 1,024, fast, 170 tiles: 16 us, in splits of 4 blocks 23) or, where most of the chip
+  // would be idle, 4 (1,840 x 106 x 2,048, 15 tiles: 17 us, with 8 blocks 23).
+  const int at_once = pl.tile == 256 ? 256 : 512;
   int splits = 1;
-  while (tiles * splits <= 256 && kb / (splits * 2) >= 4) splits *= 2;
+  while (tiles * splits * 2 <= at_once && kb / (splits * 2) >= (tiles * splits < 64 ? 4 : 8)) splits *= 2;
   pl.blocks_per_split = ceil_div(kb, splits);
   pl.splits = ceil_div(kb, pl.blocks_per_split);
   return pl;
