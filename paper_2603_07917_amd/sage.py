@@ -513,6 +513,9 @@ def _result(out: Optional[torch.Tensor], shape, dtype, like: torch.Tensor, name:
 
 
 def _scratch(workspace: Optional[torch.Tensor], need: int, device) -> Optional[torch.Tensor]:
+    """`workspace`, or a new one where it is too small."""
+    if workspace is not None and not (workspace.device == device and workspace.is_contiguous()):
+        raise SageError(f"workspace must be contiguous and on {device}")
     if need == 0 or (workspace is not None and workspace.numel() * workspace.element_size() >= need):
         return workspace
     return torch.empty(need, dtype=torch.uint8, device=device)

@@ -106,3 +106,14 @@ def test_python_refuses_host_tensors_and_shapes():
                  lambda: sage.matmul_fp8(x, x, x, x)):
         with pytest.raises(sage.SageError):
             call()
+
+
+def test_python_refuses_workspaces_elsewhere():
+    import torch
+    here, meta = torch.device("cpu"), torch.empty(64, dtype=torch.uint8, device="meta")
+    ws = torch.empty(64, dtype=torch.uint8)
+    assert sage._scratch(ws, 64, here) is ws and sage._scratch(ws, 65, here).numel() == 65
+    for bad in (meta, torch.empty(128, dtype=torch.uint8)[::2]):
+        for need in (0, 64):
+            with pytest.raises(sage.SageError):
+                sage._scratch(bad, need, here)
