@@ -7,7 +7,7 @@
 //   u = g dy, grad_x = w u - s w^3 / d sum(u s) + grad_total,
 //   grad_gain = sum over rows of dy s w.
 // Both read a row once into registers (8 columns a lane and step) and are
-// bound by the memory's rate: 16,384 x 768 bf16 with residual and 8-bit output 21 us
+// bound by the memory's rate: 16,384 x 1,024 bf16 with residual and 8-bit output 21 us
 // (118 MB, 5.5 TB/s; a large copy moves 5.0), its gradient 25.7 us (134 MB, 5.2 TB/s)
 // and 4.7 us for the gain's. 8 rows: 3.4 us, the launch and one round of loads.
 #include "sage_encode.hpp"
@@ -139,7 +139,7 @@ hipError_t norm_by_out(const void* x, const void* residual, int M, int d, const 
 // A workgroup takes kRows rows at a time and every gridDim.x-th such
 // group, and keeps its columns' sums of dy s w in registers; each workgroup's
 // sums go to a row of `part`, which norm_gain_kernel adds in a fixed order.
-// At most this many rows of partial sums (16,384 x 768, both kernels: 1,024 41 us
+// At most this many rows of partial sums (16,384 x 1,024, both kernels: 1,024 41 us
 // between events, 512 55, 768 46, 2,048 46).
 constexpr int kGradGroups = 1024;
 
